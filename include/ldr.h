@@ -44,7 +44,8 @@ enum ldr_status {
   LDR_ERANGE = -2,  /* a per-sequence row count outside [0, max_new]        */
   LDR_EHIP = -3,    /* a HIP runtime call or kernel launch failed           */
   LDR_ENOMEM = -4,  /* the small host/device bookkeeping allocation failed  */
-  LDR_ESCRATCH = -5 /* the call needs more than the static scratch holds    */
+  LDR_ESCRATCH = -5,/* the call needs more than the static scratch holds    */
+  LDR_EPAGES = -6   /* a sequence found no room in the page pool or its table */
 };
 
 enum ldr_dtype { LDR_F32 = 0, LDR_BF16 = 1 };
@@ -241,9 +242,160 @@ int ldr_views_update_ws(ldr_views* v, const int32_t* n_new, int32_t max_new, con
  * 0). Clears the status if `clear` is nonzero. */
 int ldr_views_status(ldr_views* v, int clear, void* stream);
 
+/* Copies and resets whole sequences of the views, as a serving batch does when
+ * a prompt is sampled several times or a slot goes to another request.
+ * Sequence b takes the views and the position of sequence src[b]; src[b] = b
+ * leaves it as it is, src[b] = -1 resets it to the empty state of
+ * ldr_views_init. A source has to keep its own views in the same call
+ * (src[src[b]] == src[b]); otherwise, and for an entry outside [-1, batch),
+ * sequence b stays as it is and the sticky LDR_ERANGE flag is set. Ordered with
+ * the handle's other calls as ldr_views_update is.
+ *   src  dev int32 [batch] */
+int ldr_views_fork(ldr_views* v, const int32_t* src, void* stream);
+
 /* Frees the handle and its status word; the arena, pos and G stay the
  * caller's. NULL is ignored. */
 void ldr_views_destroy(ldr_views* v);
+
+/* ---- Paged K/V cache --------------------------------------------------------
+ * The K/V rows that verification passes attend to and the views are made from,
+ * in pages that sequences can share. Everything that changes from round to
+ * round (lengths, page tables, reference counts) is device memory and is
+ * changed by kernels, so a round needs no host value: its rows are reserved and
+ * written, attended to, and cut back by the counts that a verification wrote.
+ *
+ *   pool   dev [n_layers][2][n_pages][n_kv_heads][page * head_dim] dtype: per
+ *          layer the K pages, each head's rows [page][head_dim], then the V
+ *          pages, each head's rows transposed, [head_dim][page]
+ *   state  dev int32 words, ldr_pages_state_bytes(cfg) bytes:
+ *          rows [batch]   rows of each sequence
+ *          open [batch]   how many of them, at the end, are open: reserved by
+ *                         the last ldr_pages_reserve and not shared since
+ *          table [batch][max_pages]  page of rows [j page, (j + 1) page); -1
+ *                         where the sequence has none
+ *          refs [n_pages] tables holding each page; 0: free
+ *          at ldr_pages_layout's offsets, before and behind them words of the
+ *          library. A copy of the whole state, put back later, undoes what
+ *          calls in between did to the tables, not to the pool.
+ *
+ * Calls on one handle must be ordered (one stream, or streams joined by
+ * events), and run with the device current that holds its memory. A table
+ * entry or a length that is out of range (only a caller's own writes can leave
+ * one) is clamped where it is read. */
+typedef struct ldr_pages_config {
+  int32_t n_layers;      /* layers in the pool                                */
+  int32_t n_kv_heads;
+  int32_t head_dim;      /* 64 or 128                                         */
+  int32_t page;          /* rows of a page: 32, 64, 128 or 256                */
+  int32_t n_pages;       /* pages of the pool                                 */
+  int32_t batch;         /* sequences, 1 .. 1024                              */
+  int32_t max_pages;     /* pages of a sequence; max_pages * page < 2^30      */
+  int32_t dtype;         /* enum ldr_dtype of the pool                        */
+} ldr_pages_config;
+
+typedef struct ldr_pages ldr_pages; /* opaque host handle */
+
+/* Bytes of the pool and of the state; 0 for an invalid configuration. */
+size_t ldr_pages_pool_bytes(const ldr_pages_config* cfg);
+size_t ldr_pages_state_bytes(const ldr_pages_config* cfg);
+
+/* Byte offsets of rows, open, table and refs in the state. LDR_OK or LDR_EINVAL. */
+int ldr_pages_layout(const ldr_pages_config* cfg, size_t offsets[4]);
+
+/* Creates a handle over a caller-owned pool and state (kept in the handle, both
+ * 256-byte aligned) and enqueues the reset to the empty cache: no rows, every
+ * page free. The pool is not written. The handle is host memory only. */
+int ldr_pages_init(ldr_pages** out, const ldr_pages_config* cfg, void* pool, void* state,
+                   void* stream);
+
+/* Makes room for n_new[b] more rows of every sequence b; these rows are its open
+ * rows from here on (n_new[b] = 0: it has none). Free pages are taken lowest
+ * first, in the order of the sequences. A sequence whose last page is part
+ * filled and held by another table too first gets a page of its own with the
+ * same contents in every layer (each sharer that reserves at the same time
+ * does). A sequence whose n_new is outside [0, max_new] (sticky LDR_ERANGE), or
+ * that finds no room in its table or in the pool (sticky LDR_EPAGES), keeps its
+ * rows and has no open ones; where the pool runs out, so do the sequences
+ * behind it that need a page.
+ *   n_new  dev int32 [batch] */
+int ldr_pages_reserve(ldr_pages* p, const int32_t* n_new, int32_t max_new, void* stream);
+
+/* Writes the open rows of every sequence in layers [layer, layer + n_layers):
+ * row r of K and V (r < min(open[b], max_new)) is the sequence's row
+ * rows[b] - open[b] + r. max_new is the reserve's. With all layers these are the
+ * K_new and V_new of ldr_views_update.
+ *   K, V  dev [batch][max_new][n_layers][n_kv_heads][head_dim] dtype */
+int ldr_pages_write(ldr_pages* p, int32_t layer, int32_t n_layers, const void* K, const void* V,
+                    int32_t max_new, void* stream);
+
+/* Keeps the first kept[b] open rows of every sequence and drops those behind
+ * them, as a verification decides (its n_new); the kept ones stay open. Pages
+ * without a row left are released. A count outside [0, open[b]] leaves the
+ * sequence as it is and sets the sticky LDR_ERANGE flag.
+ *   kept  dev int32 [batch] */
+int ldr_pages_keep(ldr_pages* p, const int32_t* kept, void* stream);
+
+/* Sequence b gives its pages back and takes those of sequence src[b], which both
+ * then hold; src[b] = b leaves it as it is, src[b] = -1 leaves it empty. Sources
+ * and copies have no open rows afterwards. A source has to keep its own pages in
+ * the same call (src[src[b]] == src[b]); otherwise, and for an entry outside
+ * [-1, batch), sequence b stays as it is and the sticky LDR_ERANGE flag is set.
+ *   src  dev int32 [batch] */
+int ldr_pages_fork(ldr_pages* p, const int32_t* src, void* stream);
+
+/* Moves the live pages together: with n pages in use, those with an id of n or
+ * more go to the free ids below n, both in ascending order, in every layer, and
+ * the tables follow. Pages from n on are then free and hold what they held. */
+int ldr_pages_compact(ldr_pages* p, void* stream);
+
+/* Waits for `stream` and returns the sticky device status: LDR_OK, LDR_ERANGE,
+ * LDR_EPAGES, or LDR_EINVAL once an ldr_attend ran on a plan that was not of the
+ * cache's present state (the first of them that is set). Clears it if `clear` is
+ * nonzero. */
+int ldr_pages_status(ldr_pages* p, int clear, void* stream);
+
+/* Frees the handle; pool and state stay the caller's. NULL is ignored. */
+void ldr_pages_destroy(ldr_pages* p);
+
+/* Workspace bytes of ldr_attend_plan and of the ldr_attend calls that follow it
+ * (0 for an invalid configuration or size: n_q_heads is a multiple of
+ * n_kv_heads; batch * max_new * n_q_heads < 2^28). */
+size_t ldr_attend_workspace_bytes(const ldr_pages_config* cfg, int32_t n_q_heads,
+                                  int32_t max_new);
+
+/* Plans the attention of the open rows over the cache as it is now; one plan
+ * serves every layer, until a call on the handle changes the cache. Sequences
+ * with the same groups[b] >= 0 (a negative one: alone; NULL: the sequences whose
+ * first page is the same one) read the pages that all of them have in common at
+ * the front of their tables once, for all their rows together. Which sequences
+ * share a group changes the order of the sums, nothing else.
+ *   groups     dev int32 [batch] or NULL
+ *   max_new    rows per sequence of the queries, as reserved
+ *   workspace  dev, ldr_attend_workspace_bytes(cfg, n_q_heads, max_new) bytes,
+ *              256-byte aligned; keeps the plan, and the partial results of the
+ *              ldr_attend calls on it (which must be ordered) */
+int ldr_attend_plan(const ldr_pages* p, int32_t n_q_heads, int32_t max_new,
+                    const int32_t* groups, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/* Causal attention of every open row over its sequence's rows in one layer:
+ * the query of open row i of sequence b is at position P = rows[b] - open[b] + i,
+ *   o = sum_{k <= P} exp(s_k - lse) v_k,  s_k = scale q . k_k,
+ *   lse = log sum_{k <= P} exp(s_k),
+ * query head h over K/V head h / (n_q_heads / n_kv_heads). Products in the
+ * cache's dtype, the probabilities rounded to it before they meet v; scores, sums
+ * and the joining of partial results are fp32. A row that no key's score reaches
+ * (all of them -inf) gives o = 0 and lse = -inf. What masked places hold does
+ * not count, infinities and NaN included. Rows i >= open[b] of o and lse stay as
+ * they were. n_q_heads and max_new are the plan's.
+ *   q    dev dtype, row (b, i) at q + (b max_new + i) q_stride elements, its
+ *        [n_q_heads][head_dim] contiguous; q_stride a multiple of 8 (bf16) or 4
+ *   o    dev [batch][max_new][n_q_heads][head_dim] dtype
+ *   lse  dev fp32 [batch][max_new][n_q_heads], or NULL
+ *   scale  finite and above 0 (1 / sqrt(head_dim) as a rule) */
+int ldr_attend(const ldr_pages* p, int32_t layer, const void* q, int64_t q_stride,
+               int32_t n_q_heads, int32_t max_new, float scale, void* o, float* lse,
+               void* workspace, size_t workspace_bytes, void* stream);
 
 /* One block proposal (Eq. 4; Sec. 2.3; App. A.1): base logits z^(0) of the B
  * slots of every sequence, from the views alone.
@@ -438,6 +590,42 @@ int ldr_verify(const float* target_logits, const float* draft_logits, const floa
                float temperature, int32_t top_k, uint64_t seed, uint64_t step,
                int32_t* accepted, int32_t* next_token, int32_t* n_new, void* workspace,
                size_t workspace_bytes, void* stream);
+
+/* Workspace bytes ldr_verify_probs needs (0 on a non-positive size). */
+size_t ldr_verify_probs_workspace_bytes(int32_t batch, int32_t block, int32_t vocab);
+
+/* Speculative verification (Eq. 1-2) from probabilities and random numbers that
+ * the caller has: a target row that was cut or mixed before (top-p, min-p, a
+ * grammar), draws that are replayed or come from another generator. ldr_verify
+ * is the form for logits and the library's own noise.
+ * Candidates are tested in order: y_i (i = 1 .. n_draft[b]) is accepted while
+ * u_{i-1} q_i(y_i) < p_i(y_i), a product of two fp32 numbers compared exactly; a
+ * candidate outside [0, vocab) is rejected. At the first rejection the round
+ * emits a token of w = [p_i - q_i]_+ (of p_i where w has no positive entry),
+ * after n_draft[b] acceptances one of w = p_{n_draft[b] + 1}, by inverting the
+ * cumulative sum: the first token with w_v > 0 and C_v > u_block C_{vocab - 1},
+ * C_v = w_0 + .. + w_v; where there is none (u_block >= 1, NaN) the last token
+ * with w_v > 0, and 0 for a row without one. Differences and sums are fp64, so
+ * that a draw does not depend on their order; entries of w that are not finite
+ * and above 0 count as 0. Probabilities need not sum to 1.
+ *   target_probs dev fp32 [batch][block + 1][vocab]
+ *   draft_probs  dev fp32 [batch][block][vocab]; NULL for proposals without a
+ *                distribution (drafted greedily or looked up): q_i is 1 at y_i
+ *   draft_tokens dev int32 [batch][block]
+ *   n_draft      dev int32 [batch], drafted tokens of each sequence, clamped to
+ *                [0, block]; NULL: block
+ *   uniforms     dev fp32 [batch][block + 1], in [0, 1): one for each candidate,
+ *                the last of a row for its emitted token
+ *   accepted, next_token, n_new  dev int32 [batch], as ldr_verify's
+ *   workspace    dev, ldr_verify_probs_workspace_bytes(batch, block, vocab)
+ *                bytes, 16-byte aligned
+ * LDR_EINVAL on a NULL pointer, a non-positive size, a vocab above 2^30 or a
+ * short or misaligned workspace. */
+int ldr_verify_probs(const float* target_probs, const float* draft_probs,
+                     const int32_t* draft_tokens, const int32_t* n_draft, const float* uniforms,
+                     int32_t batch, int32_t block, int32_t vocab, int32_t* accepted,
+                     int32_t* next_token, int32_t* n_new, void* workspace,
+                     size_t workspace_bytes, void* stream);
 
 /* Writes Gumbel noise of the samplers' layout: out[r][e] = -log(-log(u)) of
  * entry e of row r in noise stream noise_stream (0: ldr_sample's token noise

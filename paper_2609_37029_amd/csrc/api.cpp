@@ -1,8 +1,8 @@
 // Host side of the C ABI: configuration checks, the per-sequence arena
 // layout, the workspace plan of one draft step, argument validation and the
 // launch sequence. Every step of the drafting computation runs in the HIP
-// kernels of views.hip, gemm.hip, draft.hip, attn.hip, sample.hip and
-// verify.hip.
+// kernels of views.hip, gemm.hip, draft.hip, attn.hip, sample.hip, verify.hip
+// and verify_probs.hip. The paged cache has its host side in api_pages.cpp.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -195,6 +195,7 @@ const char* ldr_strerror(int status) {
     case LDR_ERANGE: return "row count out of range";
     case LDR_EHIP: return "HIP runtime error";
     case LDR_ENOMEM: return "out of memory";
+    case LDR_EPAGES: return "no room in the page pool or a sequence's page table";
     case LDR_ESCRATCH: return "request exceeds the static scratch of the allocation-free call";
     default: return "unknown status";
   }
@@ -283,6 +284,13 @@ int ldr_views_update_ws(ldr_views* v, const int32_t* n_new, int32_t max_new, con
                         size_t workspace_bytes, void* stream) {
   return views_update_impl(v, n_new, max_new, K_new, V_new, h_new, workspace, workspace_bytes,
                            static_cast<hipStream_t>(stream));
+}
+
+int ldr_views_fork(ldr_views* v, const int32_t* src, void* stream) {
+  if (!v || !src || !aligned(src, 4)) return LDR_EINVAL;
+  return launch_views_fork(v->s, v->L, v->batch, v->arena, v->pos, src, v->status,
+                           static_cast<hipStream_t>(stream)) == hipSuccess
+             ? LDR_OK : LDR_EHIP;
 }
 
 int ldr_views_status(ldr_views* v, int clear, void* stream) {
@@ -643,6 +651,29 @@ int ldr_verify(const float* target_logits, const float* draft_logits, const floa
   return launch_verify(target_logits, draft_logits, draft_tokens, draft_lse, batch, block, vocab,
                        temperature, top_k, seed, step, accepted, next_token, n_new, workspace,
                        static_cast<hipStream_t>(stream)) == hipSuccess
+             ? LDR_OK : LDR_EHIP;
+}
+
+size_t ldr_verify_probs_workspace_bytes(int32_t batch, int32_t block, int32_t vocab) {
+  if (batch <= 0 || block <= 0 || vocab <= 0 || vocab > (1 << 30)) return 0;
+  return verify_probs_workspace_bytes(batch, block, vocab);
+}
+
+int ldr_verify_probs(const float* target_probs, const float* draft_probs,
+                     const int32_t* draft_tokens, const int32_t* n_draft, const float* uniforms,
+                     int32_t batch, int32_t block, int32_t vocab, int32_t* accepted,
+                     int32_t* next_token, int32_t* n_new, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  if (!target_probs || !draft_tokens || !uniforms || !accepted || !next_token || !n_new ||
+      !workspace)
+    return LDR_EINVAL;
+  if (batch <= 0 || block <= 0 || vocab <= 0 || vocab > (1 << 30)) return LDR_EINVAL;
+  if (workspace_bytes < ldr_verify_probs_workspace_bytes(batch, block, vocab) ||
+      !aligned(workspace, 16))
+    return LDR_EINVAL;
+  return launch_verify_probs(target_probs, draft_probs, draft_tokens, n_draft, uniforms, batch,
+                             block, vocab, accepted, next_token, n_new, workspace,
+                             static_cast<hipStream_t>(stream)) == hipSuccess
              ? LDR_OK : LDR_EHIP;
 }
 

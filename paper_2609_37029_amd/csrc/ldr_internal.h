@@ -170,6 +170,57 @@ hipError_t launch_views_pool(const Shape& s, const Layout& L, int batch, void* a
 hipError_t launch_views_commit(int batch, int64_t* pos, const int32_t* n_new, int max_new,
                                int32_t* status, hipStream_t st);
 
+// Copies and resets of whole sequences (Views fork).
+hipError_t launch_views_fork(const Shape& s, const Layout& L, int batch, void* arena, int64_t* pos,
+                             const int32_t* src, int32_t* status, hipStream_t st);
+
+// Paged K/V cache (pages.hip). The state is int32 words: a header, rows, open,
+// table, refs, then scratch of the calls (lists of pages).
+struct PagesShape {
+  int layers, hkv, d, page, n_pages, batch, max_pages, dtype;
+  size_t el;
+  size_t page_bytes;                 // one page of one layer's K (or V), all heads
+  size_t rows, open, table, refs;    // word offsets in the state
+  size_t list;                       // scratch: n_pages words (free pages; compaction map)
+  size_t pairs;                      // scratch: 2 max(batch, n_pages / 2 + 1) words (from, to)
+  size_t words;
+};
+// Header words of the state.
+constexpr int kPagesFlags = 0;    // sticky flags
+constexpr int kPagesVersion = 1;  // counts the calls that change the tables
+constexpr int kPagesPairs = 2;    // pairs in the scratch list (compaction)
+constexpr int kPagesHeader = 64;
+constexpr int kFlagPages = 4;     // no room in the pool or a table
+constexpr int kFlagPlan = 8;      // an attention ran on a plan of another state
+constexpr int kMaxSeqs = 1024;    // sequences of a cache: one thread each in the bookkeeping
+struct PagesPtrs { uint8_t* pool; int32_t* state; };
+hipError_t launch_pages_reset(const PagesShape& s, const PagesPtrs& p, hipStream_t st);
+hipError_t launch_pages_reserve(const PagesShape& s, const PagesPtrs& p, const int32_t* n_new,
+                                int max_new, hipStream_t st);
+hipError_t launch_pages_write(const PagesShape& s, const PagesPtrs& p, int layer, int n_layers,
+                              const void* K, const void* V, int max_new, hipStream_t st);
+hipError_t launch_pages_keep(const PagesShape& s, const PagesPtrs& p, const int32_t* kept,
+                             hipStream_t st);
+hipError_t launch_pages_fork(const PagesShape& s, const PagesPtrs& p, const int32_t* src,
+                             hipStream_t st);
+hipError_t launch_pages_compact(const PagesShape& s, const PagesPtrs& p, hipStream_t st);
+hipError_t launch_pages_clear_flags(const PagesPtrs& p, hipStream_t st);
+
+// Attention over the paged cache (attend.hip).
+size_t attend_workspace_bytes(const PagesShape& s, int hq, int max_new);
+hipError_t launch_attend_plan(const PagesShape& s, const PagesPtrs& p, int hq, int max_new,
+                              const int32_t* groups, void* ws, hipStream_t st);
+hipError_t launch_attend(const PagesShape& s, const PagesPtrs& p, int layer, const void* q,
+                         long q_stride, int hq, int max_new, float scale, void* o, float* lse,
+                         void* ws, hipStream_t st);
+
+// Verification from given probabilities and uniforms (verify_probs.hip).
+size_t verify_probs_workspace_bytes(int batch, int B, int V);
+hipError_t launch_verify_probs(const float* P, const float* Q, const int32_t* y,
+                               const int32_t* n_draft, const float* u, int batch, int B, int V,
+                               int32_t* accepted, int32_t* token, int32_t* n_new, void* ws,
+                               hipStream_t st);
+
 // GEMM (gemm.hip): C = A[M][K] . W[N][K]^T, fp32 accumulation.
 enum GemmEpi {
   EPI_STORE = 0,   // out fp32 [split][M][N] (split-K partials; split 0 only if S = 1)

@@ -39,6 +39,51 @@ views_reset_kernel(uint8_t* arena, size_t stride, size_t eta_off, size_t eta_byt
     for (int b = threadIdx.x; b < batch; b += kThreads) pos[b] = 0;
 }
 
+// Copies and resets of sequences: the workgroups of sequence b move its slot in
+// pieces of kForkPiece bytes, from the slot of src[b] or from nothing. A source
+// keeps its slot in the same launch, so no workgroup writes what another reads.
+constexpr int kForkPiece = 16384;
+
+__global__ void __launch_bounds__(kThreads)
+views_fork_kernel(uint8_t* arena, size_t stride, size_t eta_off, size_t eta_bytes, int batch,
+                  int64_t* pos, const int32_t* src, int32_t* status) {
+  const int b = blockIdx.y, from = src[b];
+  if (from == b) return;
+  const bool first = blockIdx.x == 0 && threadIdx.x == 0;
+  if (from < -1 || from >= batch || (from >= 0 && src[from] != from)) {
+    if (first) atomicOr(status, kFlagRange);
+    return;
+  }
+  const size_t off = (size_t)blockIdx.x * kForkPiece;
+  const size_t n = off + kForkPiece < stride ? kForkPiece : stride - off;   // whole 256 bytes
+  uint4* to = reinterpret_cast<uint4*>(arena + (size_t)b * stride + off);
+  constexpr int U = kForkPiece / 16 / kThreads;
+  uint4 x[U];
+  if (from >= 0) {
+    const uint4* in = reinterpret_cast<const uint4*>(arena + (size_t)from * stride + off);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const size_t i = (size_t)u * kThreads + threadIdx.x;
+      x[u] = in[i * 16 < n ? i : 0];
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {   // regions start on 256 bytes, eta ends on a word
+      const size_t at = off + ((size_t)u * kThreads + threadIdx.x) * 16;
+      uint32_t w[4];
+      for (int k = 0; k < 4; ++k)
+        w[k] = at + 4 * k >= eta_off && at + 4 * k < eta_off + eta_bytes ? 0xff800000u : 0u;
+      x[u] = uint4{w[0], w[1], w[2], w[3]};
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const size_t i = (size_t)u * kThreads + threadIdx.x;
+    if (i * 16 < n) to[i] = x[u];
+  }
+  if (first) pos[b] = from >= 0 ? pos[from] : 0;
+}
+
 // The commit of a sequence by the last of its workgroups in a launch (done ==
 // null: not this launch). Each sequence has a counter on a line of its own: one
 // counter for the whole launch takes an atomic of every workgroup in turn, which
@@ -904,6 +949,15 @@ hipError_t launch_views_reset(const Shape& s, const Layout& L, int batch, void* 
   const size_t eta_bytes = s.learned ? (size_t)s.D * s.hq * s.R * 4 : 0;
   hipLaunchKernelGGL(views_reset_kernel, dim3(blocks > 0 ? blocks : 1), dim3(kThreads), 0, st,
                      static_cast<uint8_t*>(arena), L.stride, L.eta, eta_bytes, batch, pos);
+  return hipGetLastError();
+}
+
+hipError_t launch_views_fork(const Shape& s, const Layout& L, int batch, void* arena, int64_t* pos,
+                             const int32_t* src, int32_t* status, hipStream_t st) {
+  const size_t eta_bytes = s.learned ? (size_t)s.D * s.hq * s.R * 4 : 0;
+  const dim3 grid((unsigned)((L.stride + kForkPiece - 1) / kForkPiece), batch);
+  hipLaunchKernelGGL(views_fork_kernel, grid, dim3(kThreads), 0, st, static_cast<uint8_t*>(arena),
+                     L.stride, L.eta, eta_bytes, batch, pos, src, status);
   return hipGetLastError();
 }
 

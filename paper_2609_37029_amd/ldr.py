@@ -7,6 +7,7 @@ implementation behind these names.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Dict, Optional
@@ -17,6 +18,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libldr.so")
 
 LDR_OK, LDR_EINVAL, LDR_ERANGE, LDR_EHIP, LDR_ENOMEM, LDR_ESCRATCH = 0, -1, -2, -3, -4, -5
+LDR_EPAGES = -6
 NOALLOC_SCRATCH_BYTES = 16 << 20   # LDR_NOALLOC_SCRATCH_BYTES
 LDR_F32, LDR_BF16 = 0, 1
 
@@ -52,6 +54,11 @@ class Weights(ctypes.Structure):
         ("layers", ctypes.POINTER(LayerWeights)), ("lm_head_tiled", ctypes.c_void_p)]
 
 
+class PagesConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "n_layers", "n_kv_heads", "head_dim", "page", "n_pages", "batch", "max_pages", "dtype")]
+
+
 _LIB = None
 
 
@@ -64,7 +71,7 @@ def _lib():
         L = ctypes.CDLL(LIB_PATH)
         P, I32, I64, SZ, U64 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t,
                                 ctypes.c_uint64)
-        CP = ctypes.POINTER(Config)
+        CP, PP = ctypes.POINTER(Config), ctypes.POINTER(PagesConfig)
         sig = {
             "ldr_views_state_bytes": (SZ, [CP]),
             "ldr_views_stride_bytes": (SZ, [CP]),
@@ -99,6 +106,24 @@ def _lib():
             "ldr_verify_workspace_bytes": (SZ, [I32, I32, I32]),
             "ldr_verify": (ctypes.c_int, [P, P, P, P, I32, I32, I32, ctypes.c_float, I32, U64,
                                           U64, P, P, P, P, SZ, P]),
+            "ldr_views_fork": (ctypes.c_int, [P, P, P]),
+            "ldr_pages_pool_bytes": (SZ, [PP]),
+            "ldr_pages_state_bytes": (SZ, [PP]),
+            "ldr_pages_layout": (ctypes.c_int, [PP, ctypes.POINTER(SZ)]),
+            "ldr_pages_init": (ctypes.c_int, [ctypes.POINTER(P), PP, P, P, P]),
+            "ldr_pages_reserve": (ctypes.c_int, [P, P, I32, P]),
+            "ldr_pages_write": (ctypes.c_int, [P, I32, I32, P, P, I32, P]),
+            "ldr_pages_keep": (ctypes.c_int, [P, P, P]),
+            "ldr_pages_fork": (ctypes.c_int, [P, P, P]),
+            "ldr_pages_compact": (ctypes.c_int, [P, P]),
+            "ldr_pages_status": (ctypes.c_int, [P, ctypes.c_int, P]),
+            "ldr_pages_destroy": (None, [P]),
+            "ldr_attend_workspace_bytes": (SZ, [PP, I32, I32]),
+            "ldr_attend_plan": (ctypes.c_int, [P, I32, I32, P, P, SZ, P]),
+            "ldr_attend": (ctypes.c_int, [P, I32, P, I64, I32, I32, ctypes.c_float, P, P, P, SZ,
+                                          P]),
+            "ldr_verify_probs_workspace_bytes": (SZ, [I32, I32, I32]),
+            "ldr_verify_probs": (ctypes.c_int, [P, P, P, P, P, I32, I32, I32, P, P, P, P, SZ, P]),
             "ldr_strerror": (ctypes.c_char_p, [ctypes.c_int]),
         }
         for name, (res, args) in sig.items():
@@ -154,6 +179,19 @@ def _ptr(t: Optional[torch.Tensor]):
 def _stream(stream=None):
     s = torch.cuda.current_stream() if stream is None else stream
     return ctypes.c_void_p(s.cuda_stream)
+
+
+def _take(t: torch.Tensor, shape, dtype, device, name: str):
+    """Refuses a tensor that the library would read as something else."""
+    if (tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device
+            or not t.is_contiguous()):
+        raise LdrError(LDR_EINVAL, f"{name} of {tuple(t.shape)} {t.dtype} on {t.device}, needed "
+                                   f"contiguous {tuple(shape)} {dtype} on {device}")
+
+
+def _on(stream):
+    """Memory that torch allocates (and clears) for a call on `stream`."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 class Views:
@@ -219,6 +257,12 @@ class Views:
                 return torch.empty(self._ws_bytes, dtype=torch.uint8, device=self.arena.device)
         except torch.cuda.OutOfMemoryError:
             return None
+
+    def fork(self, src: torch.Tensor):
+        """ldr_views_fork: sequence b takes the views of sequence src[b] (int32
+        [batch]); src[b] = b leaves it as it is, -1 resets it."""
+        _take(src, (self.batch,), torch.int32, self.arena.device, "src")
+        _check(_lib().ldr_views_fork(self._h, _ptr(src), _stream(self._stream)), "ldr_views_fork")
 
     def status(self, clear: bool = False) -> int:
         return _lib().ldr_views_status(self._h, int(clear), _stream(self._stream))
@@ -557,3 +601,207 @@ def draft_step_sample(views: "Views", w: "DraftWeights", anchor: torch.Tensor, t
                                         _ptr(lse), _ptr(logq), _ptr(workspace), workspace.numel(),
                                         _stream(stream)), "ldr_draft_step_sample")
     return logits, tok, lse, logq
+
+
+class Pages:
+    """A paged K/V cache of `batch` sequences (ldr_pages_*): the pool and its
+    bookkeeping, both torch tensors of this object.
+
+    rows, open [batch], table [batch][max_pages] and refs [n_pages] are int32
+    views of `state`; `pool` is [n_layers][2][n_pages][n_kv_heads][page *
+    head_dim]. A clone of `state` copied back later undoes the calls in between
+    for the tables (not for the pool)."""
+
+    def __init__(self, n_layers: int, n_kv_heads: int, head_dim: int, page: int, n_pages: int,
+                 batch: int, max_pages: int, dtype: torch.dtype = torch.bfloat16, device="cuda",
+                 stream=None):
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise LdrError(LDR_EINVAL, f"a cache of {dtype}")
+        self.cfg = PagesConfig(n_layers, n_kv_heads, head_dim, page, n_pages, batch, max_pages,
+                               LDR_BF16 if dtype == torch.bfloat16 else LDR_F32)
+        L = _lib()
+        words = L.ldr_pages_state_bytes(ctypes.byref(self.cfg)) // 4
+        if not words:
+            raise LdrError(LDR_EINVAL, "Pages")
+        self.batch, self.page, self.n_pages, self.max_pages = batch, page, n_pages, max_pages
+        self.n_layers, self.hkv, self.d, self.dtype = n_layers, n_kv_heads, head_dim, dtype
+        self.pool = torch.empty(n_layers, 2, n_pages, n_kv_heads, page * head_dim, dtype=dtype,
+                                device=device)
+        self.device = self.pool.device
+        self.state = torch.empty(words, dtype=torch.int32, device=device)
+        off = (ctypes.c_size_t * 4)()
+        _check(L.ldr_pages_layout(ctypes.byref(self.cfg), off), "ldr_pages_layout")
+        part = lambda o, n: self.state[o // 4:o // 4 + n]  # noqa: E731
+        self.rows, self.open = part(off[0], batch), part(off[1], batch)
+        self.table = part(off[2], batch * max_pages).view(batch, max_pages)
+        self.refs = part(off[3], n_pages)
+        self._h = ctypes.c_void_p()
+        self._stream = stream
+
+    def init(self):
+        """ldr_pages_init: an empty cache (the pool is not written)."""
+        self.close()
+        _check(_lib().ldr_pages_init(ctypes.byref(self._h), ctypes.byref(self.cfg),
+                                     _ptr(self.pool), _ptr(self.state), _stream(self._stream)),
+               "ldr_pages_init")
+        return self
+
+    @property
+    def handle(self):
+        return self._h
+
+    def k(self, layer: int) -> torch.Tensor:
+        """A layer's K pages [n_pages][n_kv_heads][page][head_dim]."""
+        return self.pool[layer, 0].view(self.n_pages, self.hkv, self.page, self.d)
+
+    def v(self, layer: int) -> torch.Tensor:
+        """A layer's V pages, transposed [n_pages][n_kv_heads][head_dim][page]."""
+        return self.pool[layer, 1].view(self.n_pages, self.hkv, self.d, self.page)
+
+    def reserve(self, n_new: torch.Tensor, max_new: int):
+        """ldr_pages_reserve: room for n_new[b] more rows (int32 [batch], at most
+        max_new), the sequence's open rows from here on."""
+        _take(n_new, (self.batch,), torch.int32, self.device, "n_new")
+        _check(_lib().ldr_pages_reserve(self._h, _ptr(n_new), int(max_new),
+                                        _stream(self._stream)), "ldr_pages_reserve")
+
+    def write(self, K: torch.Tensor, V: torch.Tensor, layer: int = 0):
+        """ldr_pages_write: the open rows from K and V [batch][max_new][layers]
+        [n_kv_heads][head_dim], into layers `layer` and on."""
+        shape = (self.batch, K.shape[1], K.shape[2], self.hkv, self.d) if K.dim() == 5 else ()
+        _take(K, shape, self.dtype, self.device, "K")
+        _take(V, shape, self.dtype, self.device, "V")
+        _check(_lib().ldr_pages_write(self._h, int(layer), shape[2], _ptr(K), _ptr(V), shape[1],
+                                      _stream(self._stream)), "ldr_pages_write")
+
+    def append(self, n_new: torch.Tensor, K: torch.Tensor, V: torch.Tensor):
+        """Reserve and write the rows of all layers, as Views.update takes them."""
+        if K.dim() != 5 or K.shape[2] != self.n_layers:
+            raise LdrError(LDR_EINVAL, f"append of K {tuple(K.shape)}")
+        self.reserve(n_new, K.shape[1])
+        self.write(K, V)
+
+    def keep(self, kept: torch.Tensor):
+        """ldr_pages_keep: of the open rows, the first kept[b] (int32 [batch])."""
+        _take(kept, (self.batch,), torch.int32, self.device, "kept")
+        _check(_lib().ldr_pages_keep(self._h, _ptr(kept), _stream(self._stream)), "ldr_pages_keep")
+
+    def fork(self, src: torch.Tensor):
+        """ldr_pages_fork: sequence b takes the pages of sequence src[b] (int32
+        [batch]); src[b] = b leaves it as it is, -1 leaves it empty."""
+        _take(src, (self.batch,), torch.int32, self.device, "src")
+        _check(_lib().ldr_pages_fork(self._h, _ptr(src), _stream(self._stream)), "ldr_pages_fork")
+
+    def compact(self):
+        """ldr_pages_compact: the live pages to the lowest ids."""
+        _check(_lib().ldr_pages_compact(self._h, _stream(self._stream)), "ldr_pages_compact")
+
+    def status(self, clear: bool = False) -> int:
+        return _lib().ldr_pages_status(self._h, int(clear), _stream(self._stream))
+
+    def attend_workspace_bytes(self, n_q_heads: int, max_new: int) -> int:
+        return int(_lib().ldr_attend_workspace_bytes(ctypes.byref(self.cfg), n_q_heads, max_new))
+
+    def plan(self, n_q_heads: int, max_new: int, groups: Optional[torch.Tensor] = None,
+             workspace: Optional[torch.Tensor] = None) -> "AttendPlan":
+        """ldr_attend_plan: a plan of the attention over the cache as it is now."""
+        return AttendPlan(self, n_q_heads, max_new, groups, workspace)
+
+    def close(self):
+        if self._h:
+            _lib().ldr_pages_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class AttendPlan:
+    """A plan of ldr_attend calls over one state of a cache; its workspace also
+    holds their partial results, so calls on one plan are ordered."""
+
+    def __init__(self, pages: Pages, n_q_heads: int, max_new: int,
+                 groups: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None):
+        need = pages.attend_workspace_bytes(n_q_heads, max_new)
+        if not need:
+            raise LdrError(LDR_EINVAL, f"a plan of {n_q_heads} query heads, {max_new} rows")
+        if groups is not None:
+            _take(groups, (pages.batch,), torch.int32, pages.device, "groups")
+        if workspace is None:
+            with _on(pages._stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device=pages.device)
+        _take(workspace, (workspace.numel(),), torch.uint8, pages.device, "workspace")
+        self.pages, self.n_q_heads, self.max_new = pages, n_q_heads, max_new
+        self.workspace = workspace
+        _check(_lib().ldr_attend_plan(pages.handle, n_q_heads, max_new, _ptr(groups),
+                                      _ptr(workspace), workspace.numel(),
+                                      _stream(pages._stream)), "ldr_attend_plan")
+
+
+def attend(plan: AttendPlan, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None,
+           lse: Optional[torch.Tensor] = None, scale: Optional[float] = None) -> torch.Tensor:
+    """ldr_attend: causal attention of the open rows over the cache's layer; q
+    [batch][max_new][n_q_heads][head_dim], its rows a constant stride apart.
+    Rows behind a sequence's open ones stay as they are (0 in a new `out`)."""
+    p = plan.pages
+    shape = (p.batch, plan.max_new, plan.n_q_heads, p.d)
+    if q.dim() != 4:
+        raise LdrError(LDR_EINVAL, f"q of {tuple(q.shape)}")
+    # the stride of a row (b, i), whatever torch says of dimensions of one entry
+    row = q.stride(1) if plan.max_new > 1 else q.stride(0) if p.batch > 1 else q[0, 0].numel()
+    if (tuple(q.shape) != shape or q.dtype != p.dtype or q.device != p.device
+            or not q[0, 0].is_contiguous() or (p.batch > 1 and q.stride(0) != plan.max_new * row)):
+        raise LdrError(LDR_EINVAL, f"q of {tuple(q.shape)} {q.dtype}, strides {q.stride()}")
+    if out is None:
+        with _on(p._stream):
+            out = torch.zeros(shape, dtype=p.dtype, device=p.device)
+    _take(out, shape, p.dtype, p.device, "out")
+    if lse is not None:
+        _take(lse, shape[:3], torch.float32, p.device, "lse")
+    scale = p.d ** -0.5 if scale is None else float(scale)
+    _check(_lib().ldr_attend(p.handle, int(layer), _ptr(q), row, plan.n_q_heads,
+                             plan.max_new, scale, _ptr(out), _ptr(lse), _ptr(plan.workspace),
+                             plan.workspace.numel(), _stream(p._stream)), "ldr_attend")
+    return out
+
+
+def verify_probs_workspace_bytes(batch: int, block: int, vocab: int) -> int:
+    return int(_lib().ldr_verify_probs_workspace_bytes(batch, block, vocab))
+
+
+def verify_probs(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor],
+                 draft_tokens: torch.Tensor, uniforms: torch.Tensor,
+                 n_draft: Optional[torch.Tensor] = None, out=None,
+                 workspace: Optional[torch.Tensor] = None, stream=None):
+    """ldr_verify_probs: target probabilities [batch][B + 1][V], draft
+    probabilities [batch][B][V] or None (proposals without a distribution),
+    tokens int32 [batch][B], uniforms fp32 [batch][B + 1], drafted tokens int32
+    [batch] -> (accepted, next_token, n_new), int32 [batch] each."""
+    batch, B1, V = target_probs.shape
+    B, dev = B1 - 1, target_probs.device
+    _take(target_probs, (batch, B1, V), torch.float32, dev, "target_probs")
+    if draft_probs is not None:
+        _take(draft_probs, (batch, B, V), torch.float32, dev, "draft_probs")
+    _take(draft_tokens, (batch, B), torch.int32, dev, "draft_tokens")
+    _take(uniforms, (batch, B1), torch.float32, dev, "uniforms")
+    if n_draft is not None:
+        _take(n_draft, (batch,), torch.int32, dev, "n_draft")
+    if out is None:
+        with _on(stream):
+            out = tuple(torch.empty(batch, dtype=torch.int32, device=dev) for _ in range(3))
+    for t, name in zip(out, ("accepted", "next_token", "n_new")):
+        _take(t, (batch,), torch.int32, dev, name)
+    if workspace is None:
+        with _on(stream):
+            workspace = torch.empty(verify_probs_workspace_bytes(batch, B, V), dtype=torch.uint8,
+                                    device=dev)
+    acc, tok, n_new = out
+    _check(_lib().ldr_verify_probs(_ptr(target_probs), _ptr(draft_probs), _ptr(draft_tokens),
+                                   _ptr(n_draft), _ptr(uniforms), batch, B, V, _ptr(acc),
+                                   _ptr(tok), _ptr(n_new), _ptr(workspace), workspace.numel(),
+                                   _stream(stream)), "ldr_verify_probs")
+    return out

@@ -1,0 +1,233 @@
+"""The plain forms of the paged cache, of attention over it and of the
+verification from given probabilities, against definitions, invariants and
+independent library routines on the CPU; and the refusals of the calls, which
+need no GPU."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages as OP
+
+
+def _check(c):
+    """Every page is held by as many tables as it counts, and a sequence has as
+    many pages as its rows need."""
+    held = np.zeros(c.n_pages, int)
+    for b, t in enumerate(c.table):
+        assert len(t) == -(-c.rows[b] // c.page) and len(set(t)) == len(t)
+        for p in t:
+            held[p] += 1
+        assert 0 <= c.open[b] <= c.rows[b]
+    assert np.array_equal(held, c.refs)
+
+
+def test_cache_against_lists_of_rows():
+    """A random history of calls: every sequence's rows are those of a plain list."""
+    rng = np.random.default_rng(0)
+    c = OP.Cache(2, 1, 4, 32, 24, 4, 6)
+    want = [np.zeros((0, 2, 1, 4)) for _ in range(4)]
+    for step in range(60):
+        op = rng.integers(4)
+        if op <= 1:
+            n = rng.integers(0, 20, 4)
+            K = rng.standard_normal((4, 20, 2, 1, 4))
+            c.reserve(n, 20)
+            c.write(K, -K)
+            kept = [rng.integers(0, o + 1) for o in c.open]
+            c.keep(kept)
+            want = [np.concatenate([w, K[b, :kept[b]]]) for b, w in enumerate(want)]
+        elif op == 2:
+            src = np.arange(4)
+            src[rng.integers(4)] = rng.integers(-1, 4)
+            src = [a if a < 0 or src[a] == a else b for b, a in enumerate(src)]
+            c.fork(src)
+            want = [want[a] if a >= 0 else want[0][:0] for a in src]
+        else:
+            c.compact()
+            live = sum(r > 0 for r in c.refs)
+            assert all(c.refs[:live]) and not any(c.refs[live:])
+        _check(c)
+        for b in range(4):
+            for layer in range(2):
+                K, V = c.sequence(layer, b)
+                assert np.array_equal(K, want[b][:, layer]) and np.array_equal(V, -K)
+    assert c.flags <= {OP.EPAGES}
+
+
+def test_reserve_serves_in_order_and_refuses():
+    c = OP.Cache(1, 1, 4, 32, 4, 4, 3)
+    c.reserve([32, 70, 32, 0], 70)       # 1 + 3 pages; none left for the third
+    assert c.rows == [32, 70, 0, 0] and c.open == [32, 70, 0, 0] and c.flags == {OP.EPAGES}
+    c = OP.Cache(1, 1, 4, 32, 4, 2, 2)
+    c.reserve([65, 9], 65)               # no table of three pages
+    assert c.rows == [0, 9] and c.flags == {OP.EPAGES}
+    c.reserve([-1, 66], 65)
+    assert c.rows == [0, 9] and c.open == [0, 0] and OP.ERANGE in c.flags
+
+
+def test_attend_is_causal_attention():
+    rng = np.random.default_rng(1)
+    q, K, V = (rng.standard_normal(s) for s in ((5, 4, 8), (11, 2, 8), (11, 2, 8)))
+    o, lse = OP.attend(q, K, V, 0.3)
+    t = lambda x: torch.tensor(x).permute(1, 0, 2).repeat_interleave(4 // x.shape[1], 0)  # noqa: E731
+    mask = torch.ones(5, 11, dtype=torch.bool).tril(6)
+    ref = torch.nn.functional.scaled_dot_product_attention(t(q), t(K), t(V), attn_mask=mask,
+                                                           scale=0.3)
+    np.testing.assert_allclose(o, ref.permute(1, 0, 2).numpy(), rtol=1e-12)
+    s = (t(q) @ t(K).transpose(1, 2) * 0.3).masked_fill(~mask, -np.inf)
+    np.testing.assert_allclose(lse, torch.logsumexp(s, -1).t().numpy(), rtol=1e-12)
+
+
+def test_attend_leaves_masked_values_out():
+    q, K, V = np.ones((2, 1, 4)), np.ones((3, 1, 4)), np.ones((3, 1, 4))
+    K[2], V[2] = np.nan, np.inf
+    o, lse = OP.attend(q, K, V, 0.5)
+    assert np.all(o[0] == 1) and np.isnan(o[1]).all()
+    o, lse = OP.attend(np.ones((3, 1, 4)), K[:2], V[:2], 0.5)     # a row before the first key
+    assert np.all(o[0] == 0) and lse[0, 0] == -np.inf and np.all(o[1:] == 1)
+
+
+def test_verify_probs_draws_the_target():
+    """Accept-or-redraw leaves the target's distribution whatever the draft's is:
+    frequencies within 5 standard deviations."""
+    rng = np.random.default_rng(2)
+    p, q = rng.dirichlet(np.ones(6)), rng.dirichlet(np.ones(6))
+    n, counts = 40000, np.zeros(6)
+    for _ in range(n):
+        y = rng.choice(6, p=q)
+        u = rng.random(2)
+        r, t = OP.verify_probs(np.stack([p, p]), q[None], [y], None, u)
+        counts[y if r else t] += 1
+    assert np.all(np.abs(counts - n * p) < 5 * np.sqrt(n * p * (1 - p)))
+
+
+def test_verify_probs_edges():
+    P = np.zeros((3, 4))
+    P[0], P[1], P[2] = [.5, .5, 0, 0], [0, 0, 1, 0], [.25, .25, .25, .25]
+    Q = P[:2].copy()
+    assert OP.verify_probs(P, Q, [0, 2], None, [.9, .9, .5]) == (2, 2)      # C_1 = .5 is not above
+    assert OP.verify_probs(P, Q, [0, 2], 0, [.9, .9, .5]) == (0, 1)         # no draft at all
+    assert OP.verify_probs(P, Q, [3, 2], None, [.9, .9, .2]) == (0, 0)      # residual empty: p itself
+    assert OP.verify_probs(P, Q, [-1, 2], 9, [.9, .9, .7]) == (0, 1)
+    assert OP.verify_probs(P, None, [0, 1], None, [.4, .9, .0]) == (1, 2)
+    assert OP.verify_probs(P, None, [0, 2], None, [.6, .9, .0]) == (0, 1)   # y left out
+    assert OP.verify_probs(P, Q, [0, 2], None, [.9, .9, 1.0]) == (2, 3)
+    assert OP.verify_probs(P * 0, Q, [0, 2], None, [.9, .9, .3]) == (0, 0)
+    P[2] = [np.nan, np.inf, -1, .5]
+    assert OP.verify_probs(P, Q, [0, 2], None, [.9, .9, .3]) == (2, 3)
+
+
+# ------------------------------------------------------- refusals, on the host
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2609_37029_amd import ldr
+    return ldr
+
+
+GOOD = dict(n_layers=5, n_kv_heads=8, head_dim=128, page=64, n_pages=2048, batch=16,
+            max_pages=600, dtype=1)
+
+
+def _cfg(L, **kw):
+    return L.PagesConfig(**{**GOOD, **kw})
+
+
+@pytest.mark.parametrize("bad", [
+    dict(n_layers=0), dict(n_kv_heads=0), dict(head_dim=96), dict(page=48), dict(page=512),
+    dict(n_pages=0), dict(batch=0), dict(batch=1025), dict(max_pages=0),
+    dict(max_pages=1 << 24), dict(dtype=2)])
+def test_pages_config_refusals(L, bad):
+    lib, c = L.lib(), ctypes.byref(_cfg(L, **bad))
+    assert lib.ldr_pages_pool_bytes(c) == 0 and lib.ldr_pages_state_bytes(c) == 0
+    assert lib.ldr_pages_layout(c, (ctypes.c_size_t * 4)()) == L.LDR_EINVAL
+    assert lib.ldr_attend_workspace_bytes(c, 32, 17) == 0
+    h = ctypes.c_void_p()
+    fake = ctypes.c_void_p(1 << 20)   # aligned, never dereferenced: validation fails first
+    assert lib.ldr_pages_init(ctypes.byref(h), c, fake, fake, None) == L.LDR_EINVAL and not h
+
+
+def test_pages_sizes(L):
+    lib, c = L.lib(), ctypes.byref(_cfg(L))
+    assert lib.ldr_pages_pool_bytes(c) == 5 * 2 * 2048 * 8 * 64 * 128 * 2
+    off = (ctypes.c_size_t * 4)()
+    assert lib.ldr_pages_layout(c, off) == L.LDR_OK
+    assert all(o % 256 == 0 for o in off) and list(off) == sorted(off)
+    assert off[3] - off[2] >= 16 * 600 * 4
+    assert lib.ldr_pages_state_bytes(c) >= off[3] + 2048 * 4
+    a = lib.ldr_attend_workspace_bytes(c, 32, 17)
+    assert 0 < a < lib.ldr_attend_workspace_bytes(c, 32, 512)
+    for hq, new in ((31, 17), (0, 17), (32, 0), (32, -1), (32, 1 << 24)):
+        assert lib.ldr_attend_workspace_bytes(c, hq, new) == 0
+
+
+def test_pages_host_refusals(L):
+    lib, c = L.lib(), ctypes.byref(_cfg(L))
+    E = L.LDR_EINVAL
+    h = ctypes.c_void_p()
+    fake, odd = ctypes.c_void_p(1 << 20), ctypes.c_void_p((1 << 20) + 16)
+    assert lib.ldr_pages_init(None, c, fake, fake, None) == E
+    for pool, state in ((None, fake), (fake, None), (odd, fake), (fake, odd)):
+        assert lib.ldr_pages_init(ctypes.byref(h), c, pool, state, None) == E and not h
+    assert lib.ldr_pages_reserve(None, fake, 17, None) == E
+    assert lib.ldr_pages_write(None, 0, 1, fake, fake, 17, None) == E
+    assert lib.ldr_pages_keep(None, fake, None) == E
+    assert lib.ldr_pages_fork(None, fake, None) == E
+    assert lib.ldr_pages_compact(None, None) == E
+    assert lib.ldr_pages_status(None, 0, None) == E
+    assert lib.ldr_attend_plan(None, 32, 17, None, fake, 1 << 30, None) == E
+    assert lib.ldr_attend(None, 0, fake, 4096, 32, 17, 1.0, fake, None, fake, 1 << 30, None) == E
+    assert lib.ldr_views_fork(None, fake, None) == E
+    lib.ldr_pages_destroy(None)
+    assert lib.ldr_strerror(L.LDR_EPAGES) != lib.ldr_strerror(E)
+
+
+def test_verify_probs_host_refusals(L):
+    lib = L.lib()
+    fake = ctypes.c_void_p(1 << 20)
+    need = lib.ldr_verify_probs_workspace_bytes(2, 4, 64)
+    good = [fake, fake, fake, fake, fake, 2, 4, 64, fake, fake, fake, fake, need, None]
+    assert need > 0
+    for i in (0, 2, 4, 8, 9, 10, 11):
+        assert lib.ldr_verify_probs(*good[:i], None, *good[i + 1:]) == L.LDR_EINVAL
+    for i, x in ((5, 0), (6, 0), (7, 0), (7, (1 << 30) + 1), (12, need - 1),
+                 (11, ctypes.c_void_p((1 << 20) + 8))):
+        assert lib.ldr_verify_probs(*good[:i], x, *good[i + 1:]) == L.LDR_EINVAL
+    for sizes in ((0, 4, 64), (2, 0, 64), (2, 4, 0), (2, 4, (1 << 30) + 1)):
+        assert lib.ldr_verify_probs_workspace_bytes(*sizes) == 0
+
+
+def test_binding_refuses_what_it_would_misread(L):
+    """Shapes, types and layouts: refused before the library is called."""
+    p = L.Pages(2, 2, 64, 32, 8, 3, 4, torch.float32, device="cpu")
+    i32 = torch.zeros(3, dtype=torch.int32)
+    for bad in (torch.zeros(3, dtype=torch.int64), torch.zeros(2, dtype=torch.int32),
+                torch.zeros(6, dtype=torch.int32)[::2]):
+        for call in (lambda t: p.reserve(t, 4), p.keep, p.fork,
+                     lambda t: p.plan(4, 4, groups=t)):
+            with pytest.raises(L.LdrError) as e:
+                call(bad)
+            assert e.value.code == L.LDR_EINVAL
+    K = torch.zeros(3, 4, 2, 2, 64)
+    for k, v in ((K.bfloat16(), K), (K, K.bfloat16()), (K[:2], K), (K, K[:, :3]),
+                 (K.transpose(0, 1).contiguous().transpose(0, 1), K), (K[0], K)):
+        with pytest.raises(L.LdrError):
+            p.write(k, v)
+    with pytest.raises(L.LdrError):
+        p.append(i32, K[:, :, :1], K[:, :, :1])
+    for hq, new in ((3, 4), (4, 0)):
+        with pytest.raises(L.LdrError):
+            p.plan(hq, new)
+    with pytest.raises(L.LdrError):
+        L.Pages(2, 2, 64, 32, 8, 3, 4, torch.float16, device="cpu")
+    with pytest.raises(L.LdrError):
+        L.Pages(2, 2, 80, 32, 8, 3, 4, torch.float32, device="cpu")
+    P, y, u = torch.zeros(2, 4, 9), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 4)
+    for args in ((P.double(), None, y, u), (P, P, y, u), (P, None, y.long(), u), (P, None, y, u[:1]),
+                 (P[:, :, ::2], None, y, u)):
+        with pytest.raises(L.LdrError):
+            L.verify_probs(*args)
+    with pytest.raises(L.LdrError):
+        L.verify_probs(P, None, y, u, n_draft=torch.zeros(3, dtype=torch.int32))
