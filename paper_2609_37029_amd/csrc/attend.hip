@@ -23,6 +23,9 @@ constexpr int kBook = 1024;          // threads of the plan's workgroup: one per
 constexpr int kRows = 32;            // query rows (x heads of a group) of an item
 constexpr int kKeys = 32;            // keys of a step; a page holds whole steps
 constexpr int kTarget = 1024;        // items x K/V heads aimed at
+constexpr int kWideRows = 256;       // rows of an item of the wide kernel
+constexpr int kWideFrom = 97;        // rows of a segment that go to it (bf16)
+constexpr int kWideTarget = 256;     // its items x K/V heads: one a CU
 constexpr int kMinChunk = 256;       // keys of an item, at least (but for a segment's end)
 constexpr int kMinShared = 128;      // keys in common that are worth a segment of their own
 constexpr int kNoMask = 1 << 30;
@@ -38,22 +41,32 @@ struct Item { int q0, r0, nr, seq, k0, k1, cbase, part; };
 // own chunks c, the same for its group's. qoff: its first entry in the row map.
 struct SeqInfo { int own_part, own_chunks, own_rows, qoff; int grp_part, grp_chunks, grp_rows, grp_qoff; };
 
-struct Header { int version, hq, max_new, items, rows, pad[59]; };
+// The wide kernel's items come first in the list.
+struct Header { int version, hq, max_new, items, wide, rows, pad[58]; };
 
 struct AttendWs {          // byte offsets in the workspace
   size_t map, info, items, ml, o, bytes;
-  int max_items;
+  int max_items, max_wide;
   long part_rows;          // rows of partial results, per K/V head
 };
+
+// Whether a segment of `rows` rows goes to the wide kernel.
+__host__ __device__ inline bool is_wide(const PagesShape& s, long rows) {
+  return s.dtype == LDR_BF16 && rows >= kWideFrom;
+}
 
 AttendWs plan_ws(const PagesShape& s, int hq, int max_new) {
   AttendWs w;
   const int rep = hq / s.hkv;
   const long rows = (long)s.batch * max_new * rep;
-  // every tile once, and the chunks that the cut into about kTarget items adds
-  w.max_items = (int)((long)s.batch * (((long)max_new * rep + kRows - 1) / kRows) + rows / kRows +
-                      s.batch / 2 + kTarget / s.hkv + 1);
-  w.part_rows = 2 * rows + (long)kRows * (kTarget / s.hkv + 1);
+  // every tile once, and the chunks that the cut into about the targets' items adds
+  const long tiles = (long)s.batch * (((long)max_new * rep + kRows - 1) / kRows) + rows / kRows +
+                     s.batch / 2;
+  w.max_items = (int)(tiles + kTarget / s.hkv + 1 + kWideTarget / s.hkv + 1);
+  const long wide = 2 * (rows / kWideRows + s.batch) + kWideTarget / s.hkv + 1;
+  w.max_wide = is_wide(s, rows) ? (int)(wide < w.max_items ? wide : w.max_items) : 0;
+  w.part_rows = 2 * rows + (long)kRows * (kTarget / s.hkv + 1) +
+                (long)kWideRows * (kWideTarget / s.hkv + 1);
   size_t off = sizeof(Header);
   w.map = off; off = align_up(off + (size_t)s.batch * max_new * 4);
   w.info = off; off = align_up(off + (size_t)s.batch * sizeof(SeqInfo));
@@ -101,7 +114,7 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   __shared__ long sums[kBook / 64];
   __shared__ int label[kBook], lead[kBook], opens[kBook], fulls[kBook], common[kBook],
       qoffs[kBook], members[kBook];
-  __shared__ int i_off[kBook], o_tiles[kBook], o_chunks[kBook], g_tiles[kBook], g_chunks[kBook],
+  __shared__ int w_off[kBook], kinds[kBook], i_off[kBook], o_tiles[kBook], o_chunks[kBook], g_tiles[kBook], g_chunks[kBook],
       o_part[kBook], g_part[kBook], ends[kBook], shares[kBook];
   const int b = threadIdx.x, rep = hq / s.hkv;
   const bool in = b < s.batch;
@@ -165,17 +178,31 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   // segments: own rows over own keys; the group's rows over the shared ones
   const long R = (long)open * rep, Rg = share && ld == b ? (long)gopen * rep : 0;
   const int len = rows - share;
-  const int ot = (int)ceil_div(R, kRows), gt = (int)ceil_div(Rg, kRows);
-  long work = 0, before = block_scan((long)ot * len + (long)gt * share, sums, &work);
-  const long per = max(1, kTarget / s.hkv);
-  const long chunk = max((long)kMinChunk, ceil_div(ceil_div(work, per), 64) * 64L);
-  const int oc = open ? (int)ceil_div(len, chunk) : 0, gc = Rg ? (int)ceil_div(share, chunk) : 0;
-  long n_items = 0;
-  const long ioff = block_scan((long)ot * oc + (long)gt * gc, sums, &n_items);
+  const bool ow = is_wide(s, R), gw = is_wide(s, Rg);
+  const int ot = (int)ceil_div(R, ow ? kWideRows : kRows),
+            gt = (int)ceil_div(Rg, gw ? kWideRows : kRows);
+  const long own_work = (long)ot * len, grp_work = (long)gt * share;
+  long work = 0, wide_work = 0;
+  long before = block_scan((ow ? 0 : own_work) + (gw ? 0 : grp_work), sums, &work);
+  block_scan((ow ? own_work : 0) + (gw ? grp_work : 0), sums, &wide_work);
+  const long per = max(1, kTarget / s.hkv), wide_per = max(1, kWideTarget / s.hkv);
+  const long narrow_chunk = max((long)kMinChunk, ceil_div(ceil_div(work, per), 64) * 64L);
+  const long wide_chunk = max((long)kMinChunk, ceil_div(ceil_div(wide_work, wide_per), 64) * 64L);
+  const int oc = open ? (int)ceil_div(len, ow ? wide_chunk : narrow_chunk) : 0;
+  const int gc = Rg ? (int)ceil_div(share, gw ? wide_chunk : narrow_chunk) : 0;
+  // the list: wide items, then the others, each in the order of the sequences,
+  // a sequence's own before its group's
+  const long oi = (long)ot * oc, gi = (long)gt * gc;
+  long n_items = 0, n_wide = 0;
+  const long woff = block_scan((ow ? oi : 0) + (gw ? gi : 0), sums, &n_wide);
+  const long noff = n_wide + block_scan((ow ? 0 : oi) + (gw ? 0 : gi), sums, &n_items);
+  n_items += n_wide;
   const bool direct = !share && oc == 1;
   long n_part = 0;
   before = block_scan((direct ? 0 : oc * R) + gc * Rg, sums, &n_part);
-  i_off[b] = (int)ioff;
+  w_off[b] = (int)woff;
+  i_off[b] = (int)noff;
+  kinds[b] = (ow ? 1 : 0) | (gw ? 2 : 0);
   o_tiles[b] = ot; o_chunks[b] = oc; g_tiles[b] = gt; g_chunks[b] = gc;
   o_part[b] = direct ? -1 : (int)before;
   g_part[b] = (int)(before + (direct ? 0 : oc * R));
@@ -188,7 +215,7 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
                       share ? gopen * rep : 0, qoffs[leader]};
   }
   // holds by the bounds of plan_ws; a list that would not fit is left empty
-  if (n_items > w.max_items || n_part > w.part_rows) n_items = 0;
+  if (n_items > w.max_items || n_wide > w.max_wide || n_part > w.part_rows) n_items = n_wide = 0;
   long total = 0;
   block_scan(open, sums, &total);
   if (b == 0) {
@@ -196,18 +223,21 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
     hd->hq = hq;
     hd->max_new = max_new;
     hd->items = (int)n_items;
+    hd->wide = (int)n_wide;
     hd->rows = (int)total;
   }
   for (int c = threadIdx.x >> 6; c < s.batch; c += kBook / 64)
     for (int i = threadIdx.x & 63; i < opens[c]; i += 64) map[qoffs[c] + i] = c * max_new + i;
   for (int t = b; t < (int)n_items; t += kBook) {
+    const bool wide = t < (int)n_wide;
+    const int* offs = wide ? w_off : i_off;
     int lo = 0, hi = s.batch - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (i_off[mid] <= t) lo = mid; else hi = mid - 1;
+      if (offs[mid] <= t) lo = mid; else hi = mid - 1;
     }
-    int k = t - i_off[lo];
-    const int mine = o_tiles[lo] * o_chunks[lo];
+    int k = t - offs[lo];
+    const int mine = ((kinds[lo] & 1) != 0) == wide ? o_tiles[lo] * o_chunks[lo] : 0;
     const bool g = k >= mine;
     if (g) k -= mine;
     const int tiles = g ? g_tiles[lo] : o_tiles[lo], chunks = g ? g_chunks[lo] : o_chunks[lo];
@@ -215,15 +245,18 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
     const int from = g ? 0 : shares[lo], to = g ? shares[lo] : ends[lo];
     const int seg = info[lo].own_rows;
     const int R2 = g ? info[lo].grp_rows : seg;
-    const int step = (int)(ceil_div(ceil_div(to - from, chunks), kKeys) * kKeys);   // even chunks
+    const int step = (int)(ceil_div(ceil_div(to - from, chunks), 64) * 64);   // even chunks
+    const int height = wide ? kWideRows : kRows;
     Item it;
     it.q0 = qoffs[lo];
-    it.r0 = tile * kRows;
-    it.nr = min(kRows, R2 - it.r0);
+    it.r0 = tile * height;
+    it.nr = min(height, R2 - it.r0);
     it.seq = lo;
     it.k0 = from + c * step;
     it.k1 = min(to, it.k0 + step);
     it.cbase = g ? kNoMask : ends[lo] - opens[lo];
+    // keys behind the last row's own are no work
+    it.k1 = min(it.k1, it.cbase + (it.r0 + it.nr - 1) / rep + 1);
     const int pb = g ? g_part[lo] : o_part[lo];
     it.part = pb < 0 ? -1 : pb + c * R2 + it.r0;
     items[t] = it;
@@ -252,13 +285,6 @@ template <> struct Mma<uint16_t> {
             f32_to_bf16(x[2]) | (uint32_t)f32_to_bf16(x[3]) << 16};
     *reinterpret_cast<uint2*>(o) = v;
   }
-  __device__ static bool finite(u32x4 v) {
-    bool ok = true;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      ok = ok && (v[j] & 0x7f80u) != 0x7f80u && (v[j] & 0x7f800000u) != 0x7f800000u;
-    return ok;
-  }
   __device__ static float get(u32x4 v, int j) {
     return __uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16);
   }
@@ -278,12 +304,6 @@ template <> struct Mma<float> {
   }
   __device__ static void store4(float* o, const float* x) {
     *reinterpret_cast<float4*>(o) = float4{x[0], x[1], x[2], x[3]};
-  }
-  __device__ static bool finite(u32x4 v) {
-    bool ok = true;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) ok = ok && (v[j] & 0x7f800000u) != 0x7f800000u;
-    return ok;
   }
   __device__ static float get(u32x4 v, int j) { return __uint_as_float(v[j]); }
 };
@@ -309,6 +329,52 @@ __device__ inline bool plan_ok(const AttendArgs& a) {
   return ok;
 }
 
+// The larger (the sum) of a lane's value and that of the lane 32 away.
+__device__ inline float other_half(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+__device__ inline float half_max(float x) { return fmaxf(x, other_half(x)); }
+__device__ inline float half_sum(float x) { return x + other_half(x); }
+
+// V where a mask crosses a step: keys from k1 on hold anything and count as 0. A
+// value that is not finite but masked for some rows only would reach them as
+// 0 x inf: it is taken out here (true: there was one), and add_non_finite adds
+// it to the rows that see it. `k`: the key of the fragment's first element.
+template <typename T> __device__ inline bool clean_values(u32x4& v, int k, int k1) {
+  constexpr int E = Mma<T>::E;
+#pragma unroll
+  for (int j = 0; j < E; ++j)
+    if (k + j >= k1) {
+      if constexpr (E == 8) v[j >> 1] &= j & 1 ? 0x0000ffffu : 0xffff0000u;
+      else v[j] = 0u;
+    }
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    const bool inf = !(fabsf(Mma<T>::get(v, j)) < INFINITY);
+    bad = bad || inf;
+    if constexpr (E == 8) v[j >> 1] &= !inf ? 0xffffffffu : j & 1 ? 0x0000ffffu : 0xffff0000u;
+    else v[j] = inf ? 0u : v[j];
+  }
+  return bad;
+}
+// vt: the V^T rows of a head, at the first of n keys, the first of which is k.
+template <typename T, int ND>
+__device__ inline void add_non_finite(f32x16 (&o)[ND], const T* vt, int page, int n, int k, int last,
+                                      int half) {
+  for (int j = 0; j < n && k + j <= last; ++j)
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int dim = dt * 32 + i / 4 * 8 + half * 4 + i % 4;
+        const float v = Elem<T>::load(vt + (size_t)dim * page + j);
+        if (!(fabsf(v) < INFINITY)) o[dt][i] += v;
+      }
+}
+
 // One item of one K/V head: four waves take its key steps in turn, each for all
 // of its (up to 32) rows, and join at the end. A wave holds its queries as the
 // column operand, so that S^T = K Q^T leaves each lane one query's scores: the
@@ -321,8 +387,9 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(AttendArgs a) {
   using M = Mma<T>;
   constexpr int E = M::E, NF = D / (2 * E), ND = D / 32, NP = 16 / E, W = kThreads / 64;
   if (!plan_ok(a)) return;
-  const int item = (int)(blockIdx.x / a.s.hkv), head = (int)(blockIdx.x % a.s.hkv);
-  if (item >= reinterpret_cast<const Header*>(a.ws)->items) return;
+  const Header* hd = reinterpret_cast<const Header*>(a.ws);
+  const int item = hd->wide + (int)(blockIdx.x / a.s.hkv), head = (int)(blockIdx.x % a.s.hkv);
+  if (item >= hd->items) return;
   const Item it = reinterpret_cast<const Item*>(a.ws + a.w.items)[item];
   const int32_t* map = reinterpret_cast<const int32_t*>(a.ws + a.w.map);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -395,7 +462,7 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(AttendArgs a) {
     float mx = x[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    mx = half_max(mx);
     const float mn = fmaxf(m, mx), mu = mn == -INFINITY ? 0.f : mn * c2;
     const float alpha = __builtin_amdgcn_exp2f(m * c2 - mu);
     m = mn;
@@ -412,55 +479,17 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(AttendArgs a) {
 #pragma unroll
     for (int f = 0; f < NP; ++f) pf[f] = M::pack(x + f * E);
     if (masked) {
-      // keys that no row of the sequence has hold anything: their V counts as 0.
-      // A value that is not finite but masked for some rows only would reach
-      // them as 0 x inf: it is taken out and added to the rows that see it.
-      bool clean = true;
+      bool bad = false;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-        for (int f = 0; f < NP; ++f) {
-          const int k = kb + f * 2 * E + half * E;   // of the fragment's first element
-          if (k + E > it.k1) {
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-              if (k + j >= it.k1) {
-                if constexpr (E == 8) vf[dt][f][j >> 1] &= j & 1 ? 0x0000ffffu : 0xffff0000u;
-                else vf[dt][f][j] = 0u;
-              }
-          }
-          clean = clean && M::finite(vf[dt][f]);
-        }
-      if (__ballot(!clean)) {
-        float seen[16];
-        const int lim = min(it.k1 - 1, last);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          seen[i] = kb + i / E * 2 * E + half * E + i % E <= lim ? 1.f : 0.f;
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt) {
-          f32x16 pos = {}, neg = {};
-#pragma unroll
-          for (int f = 0; f < NP; ++f) {
-            const u32x4 s1 = M::pack(seen + f * E);
-            float up[E], dn[E], fin[E];
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-              const float v = M::get(vf[dt][f], j);
-              up[j] = v != v || v == INFINITY ? 1.f : 0.f;
-              dn[j] = v != v || v == -INFINITY ? 1.f : 0.f;
-              fin[j] = up[j] + dn[j] > 0.f ? 0.f : v;
-            }
-            pos = M::run(M::pack(up), s1, pos);
-            neg = M::run(M::pack(dn), s1, neg);
-            vf[dt][f] = M::pack(fin);
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            if (pos[i] > 0.f) o[dt][i] += INFINITY;
-            if (neg[i] > 0.f) o[dt][i] -= INFINITY;
-          }
-        }
+        for (int f = 0; f < NP; ++f)
+          bad = clean_values<T>(vf[dt][f], kb + f * 2 * E + half * E, it.k1) || bad;
+      if (__any(bad)) {
+        const size_t off = (size_t)clamp_page(a.s, table[kb / a.s.page]) * a.s.page_bytes;
+        add_non_finite<T, ND>(o, reinterpret_cast<const T*>(vpool + off) + hoff +
+                                     (kb & (a.s.page - 1)),
+                              a.s.page, min(kKeys, it.k1 - kb), kb, last, half);
       }
     }
 #pragma unroll
@@ -468,7 +497,7 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(AttendArgs a) {
 #pragma unroll
       for (int f = 0; f < NP; ++f) o[dt] = M::run(vf[dt][f], pf[f], o[dt]);
   }
-  l += __shfl_xor(l, 32);
+  l = half_sum(l);
 
   // join the waves: each one's (m, l) of the 32 rows, then O scaled to the common
   // maximum and added up, D / 4 floats a thread row
@@ -518,6 +547,222 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(AttendArgs a) {
       M::store4(static_cast<T*>(a.o) + at * D + e, acc);
       if (e == 0 && a.lse) a.lse[at] = ll == 0.f ? -INFINITY : mm * a.scale + logf(ll);
     }
+  }
+}
+
+// The same for many rows: a workgroup takes 256 of them, 32 a wave, over stages
+// of 64 keys that reach all waves through LDS.
+//
+// The maximum that is taken out of a row's exponents follows the scores only
+// when they pass it by 2^kLazy, and is a whole power of two in the base of the
+// exponential: O and l then change by an exact factor, in a branch that is
+// rarely taken, and nothing is scaled stage by stage.
+//
+// A stage's K and V^T travel global memory -> registers -> LDS: loaded during
+// stage j - 2, written during j - 1 into the buffer that stage j - 2 has left,
+// read in stage j; one barrier a stage. A 16-byte chunk c of row r lies at chunk
+// c ^ (r mod chunks a row), so that reads of 32 rows and writes of whole rows
+// both spread over the banks.
+constexpr float kLazy = 8.f;
+constexpr int kWideThreads = 512;
+
+template <int D>
+__global__ void __launch_bounds__(kWideThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+attend_wide_kernel(AttendArgs a) {
+  using M = Mma<uint16_t>;
+  constexpr int NF = D / 16, ND = D / 32, NT = kWideThreads;
+  constexpr int KC = D / 8, VC = 8;                  // 16-byte chunks of a K row, a V^T row
+  constexpr int LU = 64 * KC / NT;                   // chunks a thread loads of each a stage
+  constexpr int STAGE = 64 * D * 2;                  // bytes of a stage of K (or V)
+  __shared__ alignas(1024) uint8_t sk[2 * STAGE];
+  __shared__ alignas(1024) uint8_t sv[2 * STAGE];
+  __shared__ int odd_values;
+  if (!plan_ok(a)) return;
+  const Header* hd = reinterpret_cast<const Header*>(a.ws);
+  const int item = (int)(blockIdx.x / a.s.hkv), head = (int)(blockIdx.x % a.s.hkv);
+  if (item >= hd->wide) return;
+  const Item it = reinterpret_cast<const Item*>(a.ws + a.w.items)[item];
+  const int32_t* map = reinterpret_cast<const int32_t*>(a.ws + a.w.map);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int col = lane & 31, half = lane >> 5;
+  const int32_t* table = a.p.state + a.s.table + (size_t)it.seq * a.s.max_pages;
+  const size_t plane = (size_t)2 * a.layer * a.s.n_pages * a.s.page_bytes;
+  const uint16_t* kpool = reinterpret_cast<const uint16_t*>(a.p.pool + plane) +
+                          (size_t)head * a.s.page * D;
+  const uint16_t* vpool = kpool + (size_t)a.s.n_pages * a.s.page_bytes / 2;
+  const size_t page_el = a.s.page_bytes / 2;
+
+  // the lane's query; columns behind the last row repeat it
+  const bool active = wave * 32 < it.nr;
+  if (tid == 0) odd_values = 0;
+  __syncthreads();
+  int last;
+  u32x4 qf[NF];
+  {
+    const int r = it.r0 + min(wave * 32 + col, it.nr - 1), qi = r / a.rep;
+    const uint16_t* qp = static_cast<const uint16_t*>(a.q) +
+                         (size_t)map[it.q0 + qi] * a.q_stride + (head * a.rep + r - qi * a.rep) * D;
+    last = it.cbase + qi;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) qf[f] = *reinterpret_cast<const u32x4*>(qp + (2 * f + half) * 8);
+  }
+  const int first_last = it.cbase + it.r0 / a.rep;
+  const int stages = (max(it.k1 - it.k0, 0) + 63) / 64;
+  const int full = max(0, min(it.k1, first_last + 1) - it.k0) / 64;   // stages without a mask
+
+  // the loads of a stage: K rows tid / KC + .., V^T rows tid / VC + ..
+  const int kr = tid / KC, kc = tid % KC, vr = tid / VC, vc = tid % VC;
+  int ids = 0;    // pages of 32 stages, a half stage a lane
+  auto page_of = [&](int j, int h) {
+    return (size_t)__builtin_amdgcn_readlane(ids, ((j & 31) << 1) | h) * page_el;
+  };
+  u32x4 gk[LU], gv[LU];
+  auto load = [&](int j) {
+    if ((j & 31) == 0) {
+      const int k = min(it.k0 + j * 64 + lane * 32, it.k1 - 1);
+      ids = clamp_page(a.s, table[k / a.s.page]);
+    }
+    const size_t p0 = page_of(j, 0), p1 = page_of(j, 1);
+    const int k = it.k0 + j * 64;
+#pragma unroll
+    for (int u = 0; u < LU; ++u) {
+      const int row = kr + u * (NT / KC);
+      gk[u] = *reinterpret_cast<const u32x4*>(kpool + (row < 32 ? p0 : p1) +
+                                              (size_t)((k + row) & (a.s.page - 1)) * D + kc * 8);
+    }
+    const uint16_t* vb = vpool + (vc < 4 ? p0 : p1) + ((k + vc * 8) & (a.s.page - 1));
+#pragma unroll
+    for (int u = 0; u < LU; ++u)
+      gv[u] = *reinterpret_cast<const u32x4*>(vb + (size_t)(vr + u * (NT / VC)) * a.s.page);
+  };
+  auto store = [&](int j) {
+    const int at = (j & 1) * STAGE;
+    if (j >= full) {
+      bool bad = false;
+#pragma unroll
+      for (int u = 0; u < LU; ++u)
+        bad = clean_values<uint16_t>(gv[u], it.k0 + j * 64 + vc * 8, it.k1) || bad;
+      if (bad) odd_values = 1;
+    }
+#pragma unroll
+    for (int u = 0; u < LU; ++u) {
+      const int row = kr + u * (NT / KC), vrow = vr + u * (NT / VC);
+      *reinterpret_cast<u32x4*>(sk + at + row * (2 * D) + ((kc ^ (row & (KC - 1))) << 4)) = gk[u];
+      *reinterpret_cast<u32x4*>(sv + at + vrow * 128 + ((vc ^ (vrow & (VC - 1))) << 4)) = gv[u];
+    }
+  };
+  // fragments: K rows in the order that leaves a lane 8 consecutive keys. The
+  // swizzle makes a fragment's offset that of the first with bits flipped.
+  const int mi = ((col >> 3) << 2) | (col & 3), mh = (col >> 2) & 1;
+  const int krow = mi / 8 * 16 + mh * 8 + mi % 8;
+  const uint32_t klane = krow * (2 * D) + ((half ^ (krow & (KC - 1))) << 4);
+  const uint32_t vlane = col * 128 + ((half ^ (col & (VC - 1))) << 4);
+  auto kfrag = [&](uint32_t at, int sub, int f) {
+    return *reinterpret_cast<const u32x4*>(sk + (klane ^ (at + (f << 5))) + sub * (64 * D));
+  };
+  auto vfrag = [&](uint32_t at, int dt, int f) {
+    return *reinterpret_cast<const u32x4*>(sv + (vlane ^ (at + (f << 5))) + dt * 4096);
+  };
+
+  const float c2 = a.scale * 1.44269504088896341f;
+  f32x16 o[ND] = {};
+  float mu = -INFINITY, l = 0.f;
+  if (stages > 0) {
+    load(0);
+    store(0);
+    if (stages > 1) load(1);
+  }
+  for (int j = 0; j < stages; ++j) {
+    lds_barrier();   // stage j is whole, and stage j - 1 has been read
+    if (j + 1 < stages) store(j + 1);
+    if (j + 2 < stages) load(j + 2);
+    if (!active) continue;
+    const uint32_t at = (j & 1) * STAGE;
+    f32x16 sc[2] = {};
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+      for (int f = 0; f < NF; ++f) sc[sub] = M::run(kfrag(at, sub, f), qf[f], sc[sub]);
+    if (j >= full) {
+      const int lim = min(it.k1 - 1, last) - (it.k0 + j * 64);
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (sub * 32 + i / 8 * 16 + half * 8 + i % 8 > lim) sc[sub][i] = -INFINITY;
+    }
+    float mx = fmaxf(sc[0][0], sc[1][0]);
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, fmaxf(sc[0][i], sc[1][i]));
+    mx = half_max(mx) * c2;
+    const bool up = mx > mu + kLazy;
+    if (__any(up)) {
+      const float mn = up ? ceilf(mx) : mu;
+      const float alpha = up ? __builtin_amdgcn_exp2f(mu - mn) : 1.f;
+      mu = mn;
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) o[dt] *= alpha;
+    }
+    const float z = mu == -INFINITY ? 0.f : mu;
+    u32x4 pf[4];
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(fmaf(sc[sub][i], c2, -z));
+        sum[sub] += x[i];
+      }
+#pragma unroll
+      for (int f = 0; f < 2; ++f) pf[sub * 2 + f] = M::pack(x + 8 * f);
+    }
+    l += sum[0] + sum[1];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int f = 0; f < 4; ++f) o[dt] = M::run(vfrag(at, dt, f), pf[f], o[dt]);
+  }
+  if (full < stages) {
+    lds_barrier();
+    if (odd_values)
+      for (int k = it.k0 + full * 64; k < it.k1; k += kKeys)
+        add_non_finite<uint16_t, ND>(o, vpool + clamp_page(a.s, table[k / a.s.page]) * page_el +
+                                            (k & (a.s.page - 1)),
+                                     a.s.page, min(kKeys, it.k1 - k), k, last, half);
+  }
+
+  // parts or results, straight from the registers
+  l = half_sum(l);
+  const int row = wave * 32 + col;
+  if (row >= it.nr) return;
+  const float m = mu * 0.693147180559945309f;
+  if (it.part >= 0) {
+    const size_t pr = (size_t)head * a.w.part_rows + it.part + row;
+    float* out = reinterpret_cast<float*>(a.ws + a.w.o) + pr * D + half * 4;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(out + dt * 32 + g * 8) =
+            float4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
+    if (half == 0) reinterpret_cast<float2*>(a.ws + a.w.ml)[pr] = float2{m, l};
+  } else {
+    const int rr = it.r0 + row, q = rr / a.rep;
+    const size_t at = (size_t)map[it.q0 + q] * a.hq + head * a.rep + (rr - q * a.rep);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t* out = static_cast<uint16_t*>(a.o) + at * D + half * 4;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        float x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = o[dt][4 * g + k] * inv;
+        M::store4(out + dt * 32 + g * 8, x);
+      }
+    if (half == 0 && a.lse) a.lse[at] = l == 0.f ? -INFINITY : m + logf(l);
   }
 }
 
@@ -572,6 +817,14 @@ hipError_t launch(const AttendArgs& a, hipStream_t st) {
                      dim3(kThreads), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  if constexpr (sizeof(T) == 2) {
+    if (a.w.max_wide > 0) {
+      hipLaunchKernelGGL(attend_wide_kernel<D>, dim3((unsigned)a.w.max_wide * a.s.hkv),
+                         dim3(kWideThreads), 0, st, a);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  }
   const long rows = (long)a.s.batch * a.max_new * a.hq;
   hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)((rows + 3) / 4)), dim3(kThreads),
                      0, st, a);

@@ -79,8 +79,8 @@ def test_long_cache_and_many_rows(gpu_lib):
     _run(gpu_lib, c, 4, 130)
 
 
-@pytest.mark.parametrize("dtype", [BF, F32])
-def test_masked_values_do_not_count(gpu_lib, dtype):
+@pytest.mark.parametrize("dtype,extra", [(BF, 0), (F32, 0), (BF, 80)])
+def test_masked_values_do_not_count(gpu_lib, dtype, extra):
     """NaN and infinities in the rows behind a query: later open rows, and what
     free parts of a page hold (NaN, by the test's pool). The rows that see them
     take them."""
@@ -88,20 +88,21 @@ def test_masked_values_do_not_count(gpu_lib, dtype):
         for which in ("K", "V", "KV"):
             c = Both(gpu_lib, 1, 2, 64, 32, 40, 2, 10, dtype, seed=8)
             c.append([70, 20])
-            K, V = c.rand(2, 9, 1, 2, 64), c.rand(2, 9, 1, 2, 64)
+            new = 9 + extra              # with more rows, of another kernel
+            K, V = c.rand(2, new, 1, 2, 64), c.rand(2, new, 1, 2, 64)
             if "K" in which:
                 K[0, 5] = bad
             if "V" in which:
                 V[0, 5, 0, 1, 3:40] = bad
                 V[1, 8] = bad
-            c.append([9, 9], 9, K, V)
-            q = c.rand(2, 9, 4, 64).abs() + 0.1      # K = -inf: the key has no weight
+            c.append([new, new], new, K, V)
+            q = c.rand(2, new, 4, 64).abs() + 0.1    # K = -inf: the key has no weight
             d = c.g.d
-            out = torch.zeros(2, 9, 4, d, dtype=dtype, device="cuda")
-            gpu_lib.attend(c.g.plan(4, 9), 0, q, out=out)
+            out = torch.zeros(2, new, 4, d, dtype=dtype, device="cuda")
+            gpu_lib.attend(c.g.plan(4, new), 0, q, out=out)
             torch.cuda.synchronize()
             if which == "V" or bad != bad:
-                check_attend(c, 9, q, out, None, 0, d ** -0.5)
+                check_attend(c, new, q, out, None, 0, d ** -0.5)
             else:                                    # rows before it are as if it were not there
                 assert torch.isfinite(out[0, :5]).all()
 
