@@ -7,8 +7,13 @@
 // segments (rows x keys): the rows of a group of sequences over the keys they
 // share, and the rows of each sequence over its own keys. A segment is cut into
 // tiles of rows and chunks of keys, enough items to fill the GPU. A plan kernel
-// writes the list of items (the lengths are on the device), one workgroup takes
-// an item of one K/V head, and a last kernel joins the parts of each row.
+// writes the list of items (the lengths are on the device), one workgroup of the
+// main kernel takes an item of one K/V head. Items hold whole stages of 64 keys
+// that all rows of their tile see; the keys behind them, where the mask runs
+// (fewer than 128 a tile, or all where they are few), go to the last kernel, which
+// also joins the parts of its rows.
+#include <type_traits>
+
 #include "ldr_internal.h"
 
 namespace ldr {
@@ -19,60 +24,76 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
-constexpr int kBook = 1024;          // threads of the plan's workgroup: one per sequence
-constexpr int kRows = 32;            // query rows (x heads of a group) of an item
-constexpr int kKeys = 32;            // keys of a step; a page holds whole steps
-constexpr int kTarget = 1024;        // items x K/V heads aimed at
-constexpr int kWideRows = 256;       // rows of an item of the wide kernel
-constexpr int kWideFrom = 97;        // rows of a segment that go to it (bf16)
-constexpr int kWideTarget = 256;     // its items x K/V heads: one a CU
-constexpr int kMinChunk = 256;       // keys of an item, at least (but for a segment's end)
+constexpr int kWideThreads = 512;
+constexpr int kBook = 1024;          // threads of the plan's workgroup
+constexpr int kStep = 32;            // keys of a step; a page holds whole steps
+constexpr int kStage = 64;           // keys of a stage: an item's keys are whole ones
 constexpr int kMinShared = 128;      // keys in common that are worth a segment of their own
-constexpr int kNoMask = 1 << 30;
+constexpr int kMinMain = 512;        // keys of a sequence's own that are worth items
+constexpr int kBlock = 32;           // rows of a block of partial results
+
+// Tiles of a dtype's main kernel: rows of an item, workgroups that run at once,
+// and the keys whose work an item costs on top of its own (its start, and writing
+// and joining its part).
+struct Tile { int rows, slots, cost; };
+__host__ __device__ inline Tile tile_of(const PagesShape& s) {
+  return s.dtype == LDR_BF16 ? Tile{256, 256, 384} : Tile{32, 512, 192};
+}
+// Rounds of items over the workgroups that run at once, at most.
+constexpr int kMaxRounds = 4;
 
 // One unit of work: rows r0 .. r0 + nr of a segment over keys k0 .. k1 of
 // sequence seq. Row r belongs to the segment's query r / rep, entry q0 + r / rep
-// of the row map, head r % rep of the group; it sees keys up to cbase + r / rep.
-// Its partial results go to rows part + (r - r0); part < 0: the row has no other
-// part and is finished at once.
-struct Item { int q0, r0, nr, seq, k0, k1, cbase, part; };
+// of the row map, head r % rep of the group. Partial results go to blocks of 32
+// rows from `part` on.
+struct Item { int q0, r0, nr, seq, k0, k1, part, pad; };
 
-// Parts of a sequence's rows: entries [own_part + c own_rows + own row] for its
-// own chunks c, the same for its group's. qoff: its first entry in the row map.
-struct SeqInfo { int own_part, own_chunks, own_rows, qoff; int grp_part, grp_chunks, grp_rows, grp_qoff; };
+// A sequence: its first entry in the row map, open rows, keys, and the keys it
+// leaves to its group; its own chunks of `step` keys (0: none), chunk c of its
+// row r in block own_part + c own_blocks + r / 32; the same for its group's chunks
+// and its row grp_off + r there.
+struct SeqInfo {
+  int qoff, open, rows, share, step, own_part, own_chunks, own_blocks;
+  int grp_part, grp_chunks, grp_blocks, grp_off, pad[4];
+};
+static_assert(sizeof(Item) == 32 && sizeof(SeqInfo) == 64, "read as words");
 
-// The wide kernel's items come first in the list.
-struct Header { int version, hq, max_new, items, wide, rows, pad[58]; };
+// Keys, from `share` on, that every row of the tile from row t on sees and items
+// can take: whole stages.
+__device__ inline int tile_keys(int rows, int open, int share, int t, int rep) {
+  return max(0, rows - open + t / rep + 1 - share) / kStage * kStage;
+}
+
+struct Header { int version, hq, max_new, items, pad[60]; };
 
 struct AttendWs {          // byte offsets in the workspace
   size_t map, info, items, ml, o, bytes;
-  int max_items, max_wide;
-  long part_rows;          // rows of partial results, per K/V head
+  int max_items;
+  int tiles;               // of 32 rows of a sequence
+  long blocks;             // of partial results, per K/V head
 };
 
-// Whether a segment of `rows` rows goes to the wide kernel.
-__host__ __device__ inline bool is_wide(const PagesShape& s, long rows) {
-  return s.dtype == LDR_BF16 && rows >= kWideFrom;
+// Items of one K/V head that the chunks add to a cut by tiles alone.
+__host__ __device__ inline int added_items(const PagesShape& s) {
+  return kMaxRounds * tile_of(s).slots / s.hkv + 1;
 }
 
 AttendWs plan_ws(const PagesShape& s, int hq, int max_new) {
   AttendWs w;
-  const int rep = hq / s.hkv;
+  const int rep = hq / s.hkv, tile = tile_of(s).rows;
   const long rows = (long)s.batch * max_new * rep;
-  // every tile once, and the chunks that the cut into about the targets' items adds
-  const long tiles = (long)s.batch * (((long)max_new * rep + kRows - 1) / kRows) + rows / kRows +
-                     s.batch / 2;
-  w.max_items = (int)(tiles + kTarget / s.hkv + 1 + kWideTarget / s.hkv + 1);
-  const long wide = 2 * (rows / kWideRows + s.batch) + kWideTarget / s.hkv + 1;
-  w.max_wide = is_wide(s, rows) ? (int)(wide < w.max_items ? wide : w.max_items) : 0;
-  w.part_rows = 2 * rows + (long)kRows * (kTarget / s.hkv + 1) +
-                (long)kWideRows * (kWideTarget / s.hkv + 1);
+  // every tile of the own and of the shared segments once, and the added ones
+  w.max_items = (int)((long)s.batch * (((long)max_new * rep + tile - 1) / tile) + rows / tile +
+                      s.batch / 2 + added_items(s));
+  w.tiles = (int)(((long)max_new * rep + kBlock - 1) / kBlock);
+  w.blocks = (long)s.batch * w.tiles + rows / kBlock + s.batch / 2 +
+             (long)(tile / kBlock) * added_items(s);
   size_t off = sizeof(Header);
   w.map = off; off = align_up(off + (size_t)s.batch * max_new * 4);
   w.info = off; off = align_up(off + (size_t)s.batch * sizeof(SeqInfo));
   w.items = off; off = align_up(off + (size_t)w.max_items * sizeof(Item));
-  w.ml = off; off = align_up(off + (size_t)s.hkv * w.part_rows * 8);
-  w.o = off; off = align_up(off + (size_t)s.hkv * w.part_rows * s.d * 4);
+  w.ml = off; off = align_up(off + (size_t)s.hkv * w.blocks * kBlock * 8);
+  w.o = off; off = align_up(off + (size_t)s.hkv * w.blocks * kBlock * s.d * 4);
   w.bytes = off;
   return w;
 }
@@ -108,157 +129,222 @@ __device__ inline long block_scan(long v, long* sums, long* total) {
 
 __device__ inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
 
+__device__ inline int wave_sum(int v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
+  return v;
+}
+
+// Keys of each of n even chunks of len: whole stages.
+__device__ inline int even_step(int len, int n) {
+  return ((len + n - 1) / n + kStage - 1) / kStage * kStage;
+}
+
+// The plan, in one workgroup: thread b has sequence b; what looks at all
+// sequences for each goes by waves, a sequence at a time.
 __global__ void __launch_bounds__(kBook)
 attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t* groups,
                    uint8_t* ws, AttendWs w) {
-  __shared__ long sums[kBook / 64];
-  __shared__ int label[kBook], lead[kBook], opens[kBook], fulls[kBook], common[kBook],
-      qoffs[kBook], members[kBook];
-  __shared__ int w_off[kBook], kinds[kBook], i_off[kBook], o_tiles[kBook], o_chunks[kBook], g_tiles[kBook], g_chunks[kBook],
-      o_part[kBook], g_part[kBook], ends[kBook], shares[kBook];
-  const int b = threadIdx.x, rep = hq / s.hkv;
+  constexpr int NW = kBook / 64;
+  __shared__ long sums[NW];
+  __shared__ int label[kBook], lead[kBook], opens[kBook], fulls[kBook], common[kBook];
+  __shared__ int qoffs[kBook], members[kBook], gopens[kBook];
+  __shared__ int i_off[kBook], o_chunks[kBook], g_chunks[kBook], o_part[kBook], g_part[kBook];
+  __shared__ int o_len[kBook], shares[kBook], ends[kBook];
+  __shared__ float cand_cost[NW];
+  __shared__ int cand_chunk[NW];
+  const int b = threadIdx.x, lane = b & 63, wave = b >> 6, rep = hq / s.hkv;
   const bool in = b < s.batch;
   const int32_t* table = p.state + s.table;
   Header* hd = reinterpret_cast<Header*>(ws);
   int32_t* map = reinterpret_cast<int32_t*>(ws + w.map);
   SeqInfo* info = reinterpret_cast<SeqInfo*>(ws + w.info);
   Item* items = reinterpret_cast<Item*>(ws + w.items);
+  const Tile tile = tile_of(s);
 
   const int all = in ? clamp_rows(s, p.state[s.rows + b]) : 0;
   const int held = in ? min(max(p.state[s.open + b], 0), all) : 0;
+  const int page0 = in ? clamp_page(s, table[(size_t)b * s.max_pages]) : 0;
+  const int grp = in && groups ? groups[b] : page0;
   const int open = min(held, max_new);
   const int rows = all - held + open;        // the keys that a query of the plan can see
   const int full = (all - held) / s.page;    // whole pages before the open rows
   // a sequence that has nothing to share stands alone
-  const int own = -1 - b;
-  int lb = own;
-  if (open > 0 && full > 0) {
-    if (groups) lb = groups[b] >= 0 ? groups[b] : own;
-    else lb = clamp_page(s, table[(size_t)b * s.max_pages]);
-  }
-  label[b] = lb;
+  label[b] = open > 0 && full > 0 && grp >= 0 ? grp : -1 - b;
   opens[b] = open;
   fulls[b] = full;
-  common[b] = full;
-  members[b] = 0;
   __syncthreads();
-  int ld = b;
-  if (in && lb >= 0)
-    for (int i = 0; i < b; ++i)
-      if (label[i] == lb) { ld = i; break; }
-  lead[b] = ld;
-  if (in && open > 0) atomicAdd(&members[ld], 1);
-  __syncthreads();
-  // pages in common with the first of the group, one wave per sequence
-  for (int c = threadIdx.x >> 6; c < s.batch; c += kBook / 64) {
-    const int l = lead[c];
-    if (l == c) continue;
-    const int lim = min(fulls[c], fulls[l]);
-    const int32_t* tc = table + (size_t)c * s.max_pages;
-    const int32_t* tl = table + (size_t)l * s.max_pages;
-    int same = lim;
-    for (int j = 0; j < lim; j += 64) {
-      const int k = j + (threadIdx.x & 63);
-      const uint64_t diff = __ballot(k < lim && tc[k] != tl[k]);
-      if (diff) { same = j + __builtin_ctzll(diff); break; }
+  // the first sequence of each one's group, and the size of the group
+  for (int c = wave; c < s.batch; c += NW) {
+    const int lb = label[c];
+    int first = -1, n = 0;
+    for (int i = 0; i < s.batch; i += 64) {
+      const uint64_t eq = __ballot(i + lane < s.batch && label[i + lane] == lb);
+      if (eq && first < 0) first = i + __builtin_ctzll(eq);
+      n += __builtin_popcountll(eq);
     }
-    if ((threadIdx.x & 63) == 0) atomicMin(&common[l], same);
+    if (lane == 0) {
+      lead[c] = first;
+      members[c] = n;
+      common[c] = fulls[c];
+    }
   }
   __syncthreads();
-  const int share_rows = common[ld] * s.page;
-  const int share = members[ld] > 1 && share_rows >= kMinShared ? share_rows : 0;
-  // row map: the sequences of a group behind one another
-  int qoff = 0, gopen = 0;
-  for (int i = 0; i < s.batch; ++i) {
-    const int l = lead[i], o = opens[i];
-    qoff += l < ld || (l == ld && i < b) ? o : 0;
-    gopen += l == ld ? o : 0;
+  // row map: the sequences of a group behind one another; pages in common with
+  // the first of the group, many loads at a time
+  for (int c = wave; c < s.batch; c += NW) {
+    const int ld = lead[c];
+    int before = 0, sum = 0;
+    for (int i = lane; i < s.batch; i += 64) {
+      const int l = lead[i], o = opens[i];
+      before += l < ld || (l == ld && i < c) ? o : 0;
+      sum += l == ld ? o : 0;
+    }
+    before = wave_sum(before);
+    sum = wave_sum(sum);
+    if (lane == 0) {
+      qoffs[c] = before;
+      gopens[c] = sum;
+    }
+    if (ld == c) continue;
+    const int lim = min(fulls[c], fulls[ld]);
+    const int32_t* tc = table + (size_t)c * s.max_pages;
+    const int32_t* tl = table + (size_t)ld * s.max_pages;
+    constexpr int U = 8;
+    int same = lim;
+    for (int j = 0; j < lim; j += 64 * U) {
+      int x[U], y[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = min(j + u * 64 + lane, lim - 1);
+        x[u] = tc[k];
+        y[u] = tl[k];
+      }
+      int at = lim;
+#pragma unroll
+      for (int u = U - 1; u >= 0; --u) {
+        const uint64_t diff = __ballot(x[u] != y[u]);
+        if (diff) at = min(j + u * 64 + (int)__builtin_ctzll(diff), lim);
+      }
+      if (at < lim) { same = at; break; }
+    }
+    if (lane == 0) atomicMin(&common[ld], same);
   }
-  qoffs[b] = qoff;
-  // segments: own rows over own keys; the group's rows over the shared ones
+  __syncthreads();
+  // segments: a sequence's own rows over its own keys; a group's rows, kept with
+  // its first sequence, over the shared ones
+  const int ld = in ? lead[b] : b;
+  const int common_rows = in ? common[ld] * s.page / kStage * kStage : 0;
+  const int share = in && members[b] > 1 && common_rows >= kMinShared ? common_rows : 0;
+  const int gopen = in ? gopens[b] : 0;
   const long R = (long)open * rep, Rg = share && ld == b ? (long)gopen * rep : 0;
-  const int len = rows - share;
-  const bool ow = is_wide(s, R), gw = is_wide(s, Rg);
-  const int ot = (int)ceil_div(R, ow ? kWideRows : kRows),
-            gt = (int)ceil_div(Rg, gw ? kWideRows : kRows);
-  const long own_work = (long)ot * len, grp_work = (long)gt * share;
-  long work = 0, wide_work = 0;
-  long before = block_scan((ow ? 0 : own_work) + (gw ? 0 : grp_work), sums, &work);
-  block_scan((ow ? own_work : 0) + (gw ? grp_work : 0), sums, &wide_work);
-  const long per = max(1, kTarget / s.hkv), wide_per = max(1, kWideTarget / s.hkv);
-  const long narrow_chunk = max((long)kMinChunk, ceil_div(ceil_div(work, per), 64) * 64L);
-  const long wide_chunk = max((long)kMinChunk, ceil_div(ceil_div(wide_work, wide_per), 64) * 64L);
-  const int oc = open ? (int)ceil_div(len, ow ? wide_chunk : narrow_chunk) : 0;
-  const int gc = Rg ? (int)ceil_div(share, gw ? wide_chunk : narrow_chunk) : 0;
-  // the list: wide items, then the others, each in the order of the sequences,
-  // a sequence's own before its group's
-  const long oi = (long)ot * oc, gi = (long)gt * gc;
-  long n_items = 0, n_wide = 0;
-  const long woff = block_scan((ow ? oi : 0) + (gw ? gi : 0), sums, &n_wide);
-  const long noff = n_wide + block_scan((ow ? 0 : oi) + (gw ? 0 : gi), sums, &n_items);
-  n_items += n_wide;
-  const bool direct = !share && oc == 1;
-  long n_part = 0;
-  before = block_scan((direct ? 0 : oc * R) + gc * Rg, sums, &n_part);
-  w_off[b] = (int)woff;
-  i_off[b] = (int)noff;
-  kinds[b] = (ow ? 1 : 0) | (gw ? 2 : 0);
-  o_tiles[b] = ot; o_chunks[b] = oc; g_tiles[b] = gt; g_chunks[b] = gc;
-  o_part[b] = direct ? -1 : (int)before;
-  g_part[b] = (int)(before + (direct ? 0 : oc * R));
-  ends[b] = rows;
+  const int ot = (int)ceil_div(R, tile.rows), gt = (int)ceil_div(Rg, tile.rows);
+  int len = open ? tile_keys(rows, open, share, (ot - 1) * tile.rows, rep) : 0;
+  if (len < kMinMain) len = 0;
+  const int glen = Rg ? share : 0;
+  o_len[b] = len;
   shares[b] = share;
+  ends[b] = rows;
+  long work = 0;
+  block_scan((long)ot * len + (long)gt * glen, sums, &work);
+  // The chunk: each wave tries some lengths. With slots for all items the time is
+  // a chunk's; else it is near an even spread, and half a chunk at the end.
+  {
+    const float even = (float)work * s.hkv / tile.slots;
+    const int least = max((int)min(even / kMaxRounds + 1.f, 5e8f), kStage);
+    float best = INFINITY;
+    int chunk = 0;
+    for (int t = wave; t < 4 * NW; t += NW) {
+      // from `least` to 2 x kMaxRounds of it, in even ratios
+      const float x = least * __builtin_amdgcn_exp2f(t * (3.2f / (4 * NW)));
+      const int c = (int)ceil_div((long)x, kStage) * kStage;
+      int n = 0;
+      for (int i = lane; i < s.batch; i += 64) {
+        const int l = o_len[i], o = opens[i];
+        n += ((o * rep + tile.rows - 1) / tile.rows) * ((l + c - 1) / c);
+        if (lead[i] == i && shares[i])
+          n += ((gopens[i] * rep + tile.rows - 1) / tile.rows) * ((shares[i] + c - 1) / c);
+      }
+      n = wave_sum(n);
+      const float wgs = (float)n * s.hkv;
+      const float cost = wgs <= tile.slots
+                             ? (float)c + tile.cost
+                             : ((float)work * s.hkv + wgs * tile.cost) / tile.slots +
+                                   0.5f * (c + tile.cost);
+      if (cost < best) { best = cost; chunk = c; }
+    }
+    if (lane == 0) { cand_cost[wave] = best; cand_chunk[wave] = chunk; }
+  }
+  __syncthreads();
+  int chunk = cand_chunk[0];
+  float best = cand_cost[0];
+#pragma unroll
+  for (int i = 1; i < NW; ++i)
+    if (cand_cost[i] < best) { best = cand_cost[i]; chunk = cand_chunk[i]; }
+  const int oc = (len + chunk - 1) / chunk, gc = (glen + chunk - 1) / chunk;
+  const int ob = (int)ceil_div(R, kBlock), gb = (int)ceil_div(Rg, kBlock);
+  // the list: each sequence's own items, then its group's; and the blocks of parts
+  long n_items = 0, n_part = 0;
+  const long off = block_scan((long)ot * oc + (long)gt * gc, sums, &n_items);
+  const long part = block_scan((long)oc * ob + (long)gc * gb, sums, &n_part);
+  i_off[b] = (int)off;
+  o_chunks[b] = oc; g_chunks[b] = gc;
+  o_part[b] = (int)part;
+  g_part[b] = (int)(part + (long)oc * ob);
   __syncthreads();
   if (in) {
-    const int leader = share ? ld : b;
-    info[b] = SeqInfo{o_part[b], oc, (int)R, qoff, g_part[leader], share ? g_chunks[leader] : 0,
-                      share ? gopen * rep : 0, qoffs[leader]};
+    SeqInfo f{};
+    f.qoff = qoffs[b];
+    f.open = open;
+    f.rows = rows;
+    f.share = share;
+    f.step = oc ? even_step(len, oc) : kStage;
+    f.own_part = o_part[b];
+    f.own_chunks = oc;
+    f.own_blocks = ob;
+    if (share) {
+      f.grp_part = g_part[ld];
+      f.grp_chunks = g_chunks[ld];
+      f.grp_blocks = (int)ceil_div((long)gopen * rep, kBlock);
+      f.grp_off = (qoffs[b] - qoffs[ld]) * rep;
+    }
+    info[b] = f;
   }
-  // holds by the bounds of plan_ws; a list that would not fit is left empty
-  if (n_items > w.max_items || n_wide > w.max_wide || n_part > w.part_rows) n_items = n_wide = 0;
-  long total = 0;
-  block_scan(open, sums, &total);
+  // fits by the bounds of plan_ws; a list that did not would be no plan
+  if (n_items > w.max_items || n_part > w.blocks) n_items = -1;
   if (b == 0) {
     hd->version = p.state[kPagesVersion];
     hd->hq = hq;
     hd->max_new = max_new;
     hd->items = (int)n_items;
-    hd->wide = (int)n_wide;
-    hd->rows = (int)total;
   }
-  for (int c = threadIdx.x >> 6; c < s.batch; c += kBook / 64)
-    for (int i = threadIdx.x & 63; i < opens[c]; i += 64) map[qoffs[c] + i] = c * max_new + i;
+  for (int c = wave; c < s.batch; c += NW)
+    for (int i = lane; i < opens[c]; i += 64) map[qoffs[c] + i] = c * max_new + i;
   for (int t = b; t < (int)n_items; t += kBook) {
-    const bool wide = t < (int)n_wide;
-    const int* offs = wide ? w_off : i_off;
     int lo = 0, hi = s.batch - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (offs[mid] <= t) lo = mid; else hi = mid - 1;
+      if (i_off[mid] <= t) lo = mid; else hi = mid - 1;
     }
-    int k = t - offs[lo];
-    const int mine = ((kinds[lo] & 1) != 0) == wide ? o_tiles[lo] * o_chunks[lo] : 0;
-    const bool g = k >= mine;
-    if (g) k -= mine;
-    const int tiles = g ? g_tiles[lo] : o_tiles[lo], chunks = g ? g_chunks[lo] : o_chunks[lo];
-    const int c = k / tiles, tile = k - c * tiles;
-    const int from = g ? 0 : shares[lo], to = g ? shares[lo] : ends[lo];
-    const int seg = info[lo].own_rows;
-    const int R2 = g ? info[lo].grp_rows : seg;
-    const int step = (int)(ceil_div(ceil_div(to - from, chunks), 64) * 64);   // even chunks
-    const int height = wide ? kWideRows : kRows;
+    const int own_rows = opens[lo] * rep, own_tiles = (own_rows + tile.rows - 1) / tile.rows;
+    int k = t - i_off[lo];
+    const bool g = k >= own_tiles * o_chunks[lo];
+    if (g) k -= own_tiles * o_chunks[lo];
+    const int n = g ? gopens[lo] * rep : own_rows;
+    const int tiles = (n + tile.rows - 1) / tile.rows;
+    const int c = k / tiles, r0 = (k - c * tiles) * tile.rows;
+    const int from = g ? 0 : shares[lo];
+    const int keys = g ? shares[lo] : tile_keys(ends[lo], opens[lo], from, r0, rep);
+    const int step = even_step(g ? shares[lo] : o_len[lo], g ? g_chunks[lo] : o_chunks[lo]);
     Item it;
     it.q0 = qoffs[lo];
-    it.r0 = tile * height;
-    it.nr = min(height, R2 - it.r0);
+    it.r0 = r0;
+    it.nr = min(tile.rows, n - r0);
     it.seq = lo;
     it.k0 = from + c * step;
-    it.k1 = min(to, it.k0 + step);
-    it.cbase = g ? kNoMask : ends[lo] - opens[lo];
-    // keys behind the last row's own are no work
-    it.k1 = min(it.k1, it.cbase + (it.r0 + it.nr - 1) / rep + 1);
-    const int pb = g ? g_part[lo] : o_part[lo];
-    it.part = pb < 0 ? -1 : pb + c * R2 + it.r0;
+    it.k1 = from + min(keys, (c + 1) * step);   // not above k0: the tile has no such chunk
+    it.part = (g ? g_part[lo] : o_part[lo]) + c * ((n + kBlock - 1) / kBlock) + r0 / kBlock;
+    it.pad = 0;
     items[t] = it;
   }
 }
@@ -319,12 +405,37 @@ struct AttendArgs {
   AttendWs w;
 };
 
+// A word that an earlier launch wrote and this one only reads, at an address that
+// a wave's lanes share: a scalar load into a scalar register.
+__device__ inline int32_t scalar_word(const void* p, size_t i) {
+  return ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)p)[i];
+}
+__device__ inline Item scalar_item(const void* items, size_t i) {
+  Item it;
+  it.q0 = scalar_word(items, 8 * i); it.r0 = scalar_word(items, 8 * i + 1);
+  it.nr = scalar_word(items, 8 * i + 2); it.seq = scalar_word(items, 8 * i + 3);
+  it.k0 = scalar_word(items, 8 * i + 4); it.k1 = scalar_word(items, 8 * i + 5);
+  it.part = scalar_word(items, 8 * i + 6); it.pad = 0;
+  return it;
+}
+
+__device__ inline SeqInfo scalar_info(const void* infos, size_t i) {
+  SeqInfo f;
+  f.qoff = scalar_word(infos, 16 * i); f.open = scalar_word(infos, 16 * i + 1);
+  f.rows = scalar_word(infos, 16 * i + 2); f.share = scalar_word(infos, 16 * i + 3);
+  f.step = scalar_word(infos, 16 * i + 4); f.own_part = scalar_word(infos, 16 * i + 5);
+  f.own_chunks = scalar_word(infos, 16 * i + 6); f.own_blocks = scalar_word(infos, 16 * i + 7);
+  f.grp_part = scalar_word(infos, 16 * i + 8); f.grp_chunks = scalar_word(infos, 16 * i + 9);
+  f.grp_blocks = scalar_word(infos, 16 * i + 10); f.grp_off = scalar_word(infos, 16 * i + 11);
+  return f;
+}
+
 // Whether the workspace holds a plan of the cache's present state for these
 // sizes; a workgroup that finds none records it and leaves.
-__device__ inline bool plan_ok(const AttendArgs& a) {
-  const Header* h = reinterpret_cast<const Header*>(a.ws);
-  const bool ok = h->version == a.p.state[kPagesVersion] && h->hq == a.hq &&
-                  h->max_new == a.max_new && h->items >= 0 && h->items <= a.w.max_items;
+__device__ inline bool plan_ok(const AttendArgs& a, int items) {
+  const bool ok = scalar_word(a.ws, 0) == scalar_word(a.p.state, kPagesVersion) &&
+                  scalar_word(a.ws, 1) == a.hq && scalar_word(a.ws, 2) == a.max_new &&
+                  items >= 0 && items <= a.w.max_items;
   if (!ok && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.p.state + kPagesFlags, kFlagPlan);
   return ok;
 }
@@ -375,22 +486,50 @@ __device__ inline void add_non_finite(f32x16 (&o)[ND], const T* vt, int page, in
       }
 }
 
-// One item of one K/V head: four waves take its key steps in turn, each for all
-// of its (up to 32) rows, and join at the end. A wave holds its queries as the
-// column operand, so that S^T = K Q^T leaves each lane one query's scores: the
-// softmax is lane-local but for one exchange between the halves, and the scores
-// become the column operand of O^T = V^T P^T where they are. The key that an
-// entry of S^T stands for is set by the row order in which K is loaded: the one
-// that makes each lane's entries the E consecutive keys of a V^T fragment.
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) attend_kernel(AttendArgs a) {
+// A block's partial results: O^T as the matrix products leave it, 16 bytes a lane
+// behind one another, and (m, l) of its rows. m is in units of the scores.
+template <int D> __device__ inline float* part_o(const AttendArgs& a, int head, long block) {
+  return reinterpret_cast<float*>(a.ws + a.w.o) + (head * a.w.blocks + block) * kBlock * D;
+}
+__device__ inline float2* part_ml(const AttendArgs& a, int head, long block) {
+  return reinterpret_cast<float2*>(a.ws + a.w.ml) + (head * a.w.blocks + block) * kBlock;
+}
+
+// 32 rows of one K/V head: four waves take the steps of 32 keys in turn, each for
+// all of the rows, and join at the end. A wave holds its queries as the column
+// operand, so that S^T = K Q^T leaves each lane one query's scores: the softmax is
+// lane-local but for one exchange between the halves, and the scores become the
+// column operand of O^T = V^T P^T where they are. The key that an entry of S^T
+// stands for is set by the row order in which K is loaded: the one that makes each
+// lane's entries the E consecutive keys of a V^T fragment.
+//
+// FINISH: the rows' last keys, where the mask runs; then the waves take the rows'
+// parts in turn, and the results are written. Else: an item of the f32 main
+// kernel, its results a part.
+template <typename T, int D, bool FINISH>
+__global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
   using M = Mma<T>;
   constexpr int E = M::E, NF = D / (2 * E), ND = D / 32, NP = 16 / E, W = kThreads / 64;
-  if (!plan_ok(a)) return;
-  const Header* hd = reinterpret_cast<const Header*>(a.ws);
-  const int item = hd->wide + (int)(blockIdx.x / a.s.hkv), head = (int)(blockIdx.x % a.s.hkv);
-  if (item >= hd->items) return;
-  const Item it = reinterpret_cast<const Item*>(a.ws + a.w.items)[item];
+  const int unit = (int)(blockIdx.x / a.s.hkv), head = (int)(blockIdx.x % a.s.hkv);
+  const int items = scalar_word(a.ws, 3);
+  Item it{};
+  SeqInfo f{};
+  int cbase = 0;      // row r sees keys up to cbase + r / rep
+  if constexpr (FINISH) {
+    it.seq = unit / a.w.tiles;
+    it.r0 = (unit - it.seq * a.w.tiles) * kBlock;
+    f = scalar_info(a.ws + a.w.info, it.seq);
+    if (!plan_ok(a, items) || it.r0 >= f.open * a.rep) return;
+    it.nr = min(kBlock, f.open * a.rep - it.r0);
+    it.q0 = f.qoff;
+    cbase = f.rows - f.open;
+    const int t = it.r0 / tile_of(a.s).rows * tile_of(a.s).rows;
+    it.k0 = f.share + (f.own_chunks ? tile_keys(f.rows, f.open, f.share, t, a.rep) : 0);
+    it.k1 = cbase + (it.r0 + it.nr - 1) / a.rep + 1;
+  } else {
+    it = scalar_item(a.ws + a.w.items, unit);
+    if (!plan_ok(a, items) || unit >= items || it.k1 <= it.k0) return;
+  }
   const int32_t* map = reinterpret_cast<const int32_t*>(a.ws + a.w.map);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 31, half = lane >> 5;
@@ -402,13 +541,11 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(AttendArgs a) {
 
   // the lane's query; columns behind the last row repeat it and are not stored
   const int r = it.r0 + min(col, it.nr - 1), qi = r / a.rep, hr = r - qi * a.rep;
-  const size_t qrow = map[it.q0 + qi];
+  const size_t qrow = FINISH ? (size_t)it.seq * a.max_new + qi : (size_t)map[it.q0 + qi];
   const T* qp = static_cast<const T*>(a.q) + qrow * a.q_stride + (head * a.rep + hr) * D;
-  const int last = it.cbase + qi;                      // the last key it sees
-  const int first_last = it.cbase + it.r0 / a.rep;     // the least of them in the item
   u32x4 qf[NF];
 #pragma unroll
-  for (int f = 0; f < NF; ++f) qf[f] = *reinterpret_cast<const u32x4*>(qp + (2 * f + half) * E);
+  for (int i = 0; i < NF; ++i) qf[i] = *reinterpret_cast<const u32x4*>(qp + (2 * i + half) * E);
 
   // the key of a step whose K row this lane loads
   const int mi = ((col >> 3) << 2) | (col & 3), mh = (col >> 2) & 1;
@@ -417,7 +554,7 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(AttendArgs a) {
   f32x16 o[ND] = {};
   float m = -INFINITY, l = 0.f;
 
-  const int steps = (it.k1 - it.k0 + kKeys - 1) / kKeys;
+  const int steps = (max(it.k1 - it.k0, 0) + kStep - 1) / kStep;
   int ids = 0;    // the pages of this wave's next 64 steps, one a lane
   u32x4 kf[NF];
   const T* vbase = nullptr;
@@ -425,39 +562,83 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(AttendArgs a) {
     const int st = t * W + wave;
     if ((t & 63) == 0) {
       const int sl = min((t + lane) * W + wave, steps - 1);
-      ids = clamp_page(a.s, table[(it.k0 + sl * kKeys) / a.s.page]);
+      ids = clamp_page(a.s, table[(it.k0 + sl * kStep) / a.s.page]);
     }
-    const int k = it.k0 + st * kKeys;
+    const int k = it.k0 + st * kStep;
     const size_t off = (size_t)__builtin_amdgcn_readlane(ids, t & 63) * a.s.page_bytes;
     const int in = k & (a.s.page - 1);
     const T* kp = reinterpret_cast<const T*>(kpool + off) + hoff + (size_t)(in + krow) * D;
 #pragma unroll
-    for (int f = 0; f < NF; ++f) kf[f] = *reinterpret_cast<const u32x4*>(kp + (2 * f + half) * E);
+    for (int i = 0; i < NF; ++i) kf[i] = *reinterpret_cast<const u32x4*>(kp + (2 * i + half) * E);
     vbase = reinterpret_cast<const T*>(vpool + off) + hoff + in + half * E;
   };
   if (wave < steps) fetch(0);
+  if constexpr (FINISH) {
+    // parts: the group's chunks, then the tile's own; two at a time
+    const int t = it.r0 / tile_of(a.s).rows * tile_of(a.s).rows;
+    const int own = f.own_chunks
+                        ? (tile_keys(f.rows, f.open, f.share, t, a.rep) + f.step - 1) / f.step : 0;
+    const int gr = f.grp_off + r, parts = f.grp_chunks + own;
+    constexpr int U = 2;
+    for (int c0 = wave; c0 < parts; c0 += W * U) {
+      float2 ml[U];
+      const float4* po[U];
+      float4 v[U][D / 8];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * W < parts ? c0 + u * W : c0;
+        const bool g = c < f.grp_chunks;
+        const long block = g ? f.grp_part + (long)c * f.grp_blocks + gr / kBlock
+                             : f.own_part + (long)(c - f.grp_chunks) * f.own_blocks + it.r0 / kBlock;
+        const int at = g ? gr % kBlock : r % kBlock;
+        ml[u] = part_ml(a, head, block)[at];
+        if (c0 + u * W >= parts) ml[u] = float2{-INFINITY, 0.f};
+        po[u] = reinterpret_cast<const float4*>(part_o<D>(a, head, block)) + half * 32 + at;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) v[u][i] = po[u][i * 64];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float mn = fmaxf(m, ml[u].x), mu = mn == -INFINITY ? 0.f : mn;
+        const float wo = __builtin_amdgcn_exp2f((m - mu) * c2);
+        const float wp = __builtin_amdgcn_exp2f((ml[u].x - mu) * c2);
+        const bool none = ml[u].y == 0.f;      // nothing, or a part that is not there
+        m = mn;
+        l = l * wo + ml[u].y * wp;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          const float4 x = none ? float4{} : v[u][i];
+          const int dt = i / 4, q = i % 4 * 4;
+          o[dt][q] = o[dt][q] * wo + x.x * wp;
+          o[dt][q + 1] = o[dt][q + 1] * wo + x.y * wp;
+          o[dt][q + 2] = o[dt][q + 2] * wo + x.z * wp;
+          o[dt][q + 3] = o[dt][q + 3] * wo + x.w * wp;
+        }
+      }
+    }
+    l = half ? 0.f : l;      // of both halves; the steps' sums are of one each
+  }
   for (int t = 0; t * W + wave < steps; ++t) {
-    const int kb = it.k0 + (t * W + wave) * kKeys;
+    const int kb = it.k0 + (t * W + wave) * kStep;
     u32x4 vf[ND][NP];
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-      for (int f = 0; f < NP; ++f)
-        vf[dt][f] = *reinterpret_cast<const u32x4*>(vbase + (size_t)(dt * 32 + col) * a.s.page +
-                                                    f * 2 * E);
+      for (int i = 0; i < NP; ++i)
+        vf[dt][i] = *reinterpret_cast<const u32x4*>(vbase + (size_t)(dt * 32 + col) * a.s.page +
+                                                    i * 2 * E);
     f32x16 sc = {};
 #pragma unroll
-    for (int f = 0; f < NF; ++f) sc = M::run(kf[f], qf[f], sc);
+    for (int i = 0; i < NF; ++i) sc = M::run(kf[i], qf[i], sc);
     if ((t + 1) * W + wave < steps) fetch(t + 1);
-    const bool masked = kb + kKeys > min(it.k1, first_last + 1);
     float x[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = sc[i];
-    if (masked) {
-      const int lim = min(it.k1 - 1, last);
+    if constexpr (FINISH) {
+      const int lim = cbase + qi - kb;
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (kb + i / E * 2 * E + half * E + i % E > lim) x[i] = -INFINITY;
+        if (i / E * 2 * E + half * E + i % E > lim) x[i] = -INFINITY;
     }
     float mx = x[0];
 #pragma unroll
@@ -477,30 +658,30 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(AttendArgs a) {
     for (int dt = 0; dt < ND; ++dt) o[dt] *= alpha;
     u32x4 pf[NP];
 #pragma unroll
-    for (int f = 0; f < NP; ++f) pf[f] = M::pack(x + f * E);
-    if (masked) {
+    for (int i = 0; i < NP; ++i) pf[i] = M::pack(x + i * E);
+    if (FINISH && kb + kStep > cbase + it.r0 / a.rep + 1) {
       bool bad = false;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-        for (int f = 0; f < NP; ++f)
-          bad = clean_values<T>(vf[dt][f], kb + f * 2 * E + half * E, it.k1) || bad;
+        for (int i = 0; i < NP; ++i)
+          bad = clean_values<T>(vf[dt][i], kb + i * 2 * E + half * E, it.k1) || bad;
       if (__any(bad)) {
         const size_t off = (size_t)clamp_page(a.s, table[kb / a.s.page]) * a.s.page_bytes;
         add_non_finite<T, ND>(o, reinterpret_cast<const T*>(vpool + off) + hoff +
                                      (kb & (a.s.page - 1)),
-                              a.s.page, min(kKeys, it.k1 - kb), kb, last, half);
+                              a.s.page, min(kStep, it.k1 - kb), kb, cbase + qi, half);
       }
     }
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-      for (int f = 0; f < NP; ++f) o[dt] = M::run(vf[dt][f], pf[f], o[dt]);
+      for (int i = 0; i < NP; ++i) o[dt] = M::run(vf[dt][i], pf[i], o[dt]);
   }
   l = half_sum(l);
 
   // join the waves: each one's (m, l) of the 32 rows, then O scaled to the common
-  // maximum and added up, D / 4 floats a thread row
+  // maximum and added up, four values a thread
   __shared__ float sm[W][32], sl[W][32];
   constexpr int LD = D + 4;
   __shared__ alignas(16) float so[W][32 * LD];
@@ -519,9 +700,10 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(AttendArgs a) {
           float4{o[dt][4 * g] * own, o[dt][4 * g + 1] * own, o[dt][4 * g + 2] * own,
                  o[dt][4 * g + 3] * own};
   __syncthreads();
-  const int nh = a.hq;
-  for (int i = threadIdx.x; i < it.nr * (D / 4); i += kThreads) {
-    const int row = i / (D / 4), e = (i - row * (D / 4)) * 4;
+  // thread i: values e .. e + 3 of a row; rows fastest for a part's order
+  for (int i = threadIdx.x; i < 32 * (D / 4); i += kThreads) {
+    const int row = FINISH ? i / (D / 4) : i % 32, e = FINISH ? i % (D / 4) * 4 : i / 32 * 4;
+    if (FINISH && row >= it.nr) break;
     float mm = sm[0][row];
 #pragma unroll
     for (int k = 1; k < W; ++k) mm = fmaxf(mm, sm[k][row]);
@@ -533,57 +715,70 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(AttendArgs a) {
       const float4 v = *reinterpret_cast<const float4*>(&so[k][row * LD + e]);
       acc[0] += v.x; acc[1] += v.y; acc[2] += v.z; acc[3] += v.w;
     }
-    if (it.part >= 0) {
-      const size_t pr = (size_t)head * a.w.part_rows + it.part + row;
-      *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.ws + a.w.o) + pr * D + e) =
-          float4{acc[0], acc[1], acc[2], acc[3]};
-      if (e == 0) reinterpret_cast<float2*>(a.ws + a.w.ml)[pr] = float2{mm * a.scale, ll};
-    } else {
+    if constexpr (FINISH) {
       const int rr = it.r0 + row, q = rr / a.rep;
-      const size_t at = (size_t)map[it.q0 + q] * nh + head * a.rep + (rr - q * a.rep);
+      const size_t at = ((size_t)it.seq * a.max_new + q) * a.hq + head * a.rep + (rr - q * a.rep);
       const float inv = ll == 0.f ? 0.f : 1.f / ll;
 #pragma unroll
       for (int k = 0; k < 4; ++k) acc[k] *= inv;
       M::store4(static_cast<T*>(a.o) + at * D + e, acc);
       if (e == 0 && a.lse) a.lse[at] = ll == 0.f ? -INFINITY : mm * a.scale + logf(ll);
+    } else {
+      // e = 32 dt + 8 g + 4 half
+      reinterpret_cast<float4*>(part_o<D>(a, head, it.part))[(e / 8) * 64 + (e / 4 % 2) * 32 + row] =
+          float4{acc[0], acc[1], acc[2], acc[3]};
+      if (e == 0) part_ml(a, head, it.part)[row] = float2{mm, ll};
     }
   }
 }
 
-// The same for many rows: a workgroup takes 256 of them, 32 a wave, over stages
-// of 64 keys that reach all waves through LDS.
+// The bf16 kernel: a workgroup takes an item of up to 256 rows, 32 a wave, over
+// stages of 64 keys that reach all waves through LDS.
 //
 // The maximum that is taken out of a row's exponents follows the scores only
 // when they pass it by 2^kLazy, and is a whole power of two in the base of the
 // exponential: O and l then change by an exact factor, in a branch that is
 // rarely taken, and nothing is scaled stage by stage.
 //
-// A stage's K and V^T travel global memory -> registers -> LDS: loaded during
-// stage j - 2, written during j - 1 into the buffer that stage j - 2 has left,
-// read in stage j; one barrier a stage. A 16-byte chunk c of row r lies at chunk
-// c ^ (r mod chunks a row), so that reads of 32 rows and writes of whole rows
-// both spread over the banks.
+// A stage is the products of a wave (V^T P^T of the stage before, then K Q^T:
+// 1024 cycles of the matrix unit at D = 128) and the softmax of its scores. The
+// two waves of a SIMD belong to two groups, half a stage apart: a stage has one
+// barrier, which the first group meets before its products and the second
+// before its softmax, so that one makes probabilities while the other has its
+// products.
+//
+// K and V^T go to LDS by DMA, three stages ahead, in a ring of four buffers: the
+// one of stage j has K of j and V of j - 1, which its products read between
+// barriers j and j + 1. What was read before barrier j (the buffer of j - 1) is
+// filled again right behind it, for stage j + 3; a wave waits for its share of
+// buffer j in front of barrier j. Separate arrays let the compiler see that a
+// read does not depend on the DMA in flight. A 16-byte chunk c of row r lies at
+// chunk c ^ (r mod chunks a row): reads of 32 rows spread over the banks.
 constexpr float kLazy = 8.f;
-constexpr int kWideThreads = 512;
+
+template <int N> __device__ inline void wait_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+#define LDR_GP(p) ((__attribute__((address_space(1))) void*)(p))
+#define LDR_LP(p) ((__attribute__((address_space(3))) void*)(p))
 
 template <int D>
 __global__ void __launch_bounds__(kWideThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 attend_wide_kernel(AttendArgs a) {
   using M = Mma<uint16_t>;
-  constexpr int NF = D / 16, ND = D / 32, NT = kWideThreads;
+  constexpr int NF = D / 16, ND = D / 32, NW = kWideThreads / 64;
   constexpr int KC = D / 8, VC = 8;                  // 16-byte chunks of a K row, a V^T row
-  constexpr int LU = 64 * KC / NT;                   // chunks a thread loads of each a stage
-  constexpr int STAGE = 64 * D * 2;                  // bytes of a stage of K (or V)
-  __shared__ alignas(1024) uint8_t sk[2 * STAGE];
-  __shared__ alignas(1024) uint8_t sv[2 * STAGE];
-  __shared__ int odd_values;
-  if (!plan_ok(a)) return;
-  const Header* hd = reinterpret_cast<const Header*>(a.ws);
+  constexpr int STAGE = kStage * D * 2;              // bytes of a stage of K (or V)
+  constexpr int LU = STAGE / 1024 / NW;              // DMA instructions a wave, of each a stage
+  __shared__ alignas(1024) uint8_t S0[2 * STAGE], S1[2 * STAGE], S2[2 * STAGE], S3[2 * STAGE];
   const int item = (int)(blockIdx.x / a.s.hkv), head = (int)(blockIdx.x % a.s.hkv);
-  if (item >= hd->wide) return;
-  const Item it = reinterpret_cast<const Item*>(a.ws + a.w.items)[item];
+  const int items = scalar_word(a.ws, 3);
+  const Item it = scalar_item(a.ws + a.w.items, item);
+  if (!plan_ok(a, items) || item >= items || it.k1 <= it.k0) return;
   const int32_t* map = reinterpret_cast<const int32_t*>(a.ws + a.w.map);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int32_t* table = a.p.state + a.s.table + (size_t)it.seq * a.s.max_pages;
   const size_t plane = (size_t)2 * a.layer * a.s.n_pages * a.s.page_bytes;
@@ -592,108 +787,136 @@ attend_wide_kernel(AttendArgs a) {
   const uint16_t* vpool = kpool + (size_t)a.s.n_pages * a.s.page_bytes / 2;
   const size_t page_el = a.s.page_bytes / 2;
 
-  // the lane's query; columns behind the last row repeat it
-  const bool active = wave * 32 < it.nr;
-  if (tid == 0) odd_values = 0;
-  __syncthreads();
-  int last;
+  // Up to 128 rows: both groups take the same rows, each 32 of a stage's keys,
+  // and join at the end. The lane's query; columns behind the last row repeat it.
+  const bool split = it.nr <= NW / 2 * kBlock;
+  const int block = split ? wave % (NW / 2) : wave;
+  const bool active = block * kBlock < it.nr;
   u32x4 qf[NF];
   {
-    const int r = it.r0 + min(wave * 32 + col, it.nr - 1), qi = r / a.rep;
+    const int r = it.r0 + min(block * kBlock + col, it.nr - 1), qi = r / a.rep;
     const uint16_t* qp = static_cast<const uint16_t*>(a.q) +
                          (size_t)map[it.q0 + qi] * a.q_stride + (head * a.rep + r - qi * a.rep) * D;
-    last = it.cbase + qi;
 #pragma unroll
     for (int f = 0; f < NF; ++f) qf[f] = *reinterpret_cast<const u32x4*>(qp + (2 * f + half) * 8);
   }
-  const int first_last = it.cbase + it.r0 / a.rep;
-  const int stages = (max(it.k1 - it.k0, 0) + 63) / 64;
-  const int full = max(0, min(it.k1, first_last + 1) - it.k0) / 64;   // stages without a mask
+  const int stages = (it.k1 - it.k0) / kStage;
 
-  // the loads of a stage: K rows tid / KC + .., V^T rows tid / VC + ..
-  const int kr = tid / KC, kc = tid % KC, vr = tid / VC, vc = tid % VC;
-  int ids = 0;    // pages of 32 stages, a half stage a lane
-  auto page_of = [&](int j, int h) {
-    return (size_t)__builtin_amdgcn_readlane(ids, ((j & 31) << 1) | h) * page_el;
+  // DMA. A half stage starts a page of 32, a stage lies at a multiple of 64 of a
+  // larger one: the lanes' offsets in it stay.
+  const bool small = a.s.page == 32;
+  uint32_t koff[LU], voff[LU];
+#pragma unroll
+  for (int u = 0; u < LU; ++u) {
+    const int n = wave * LU + u;
+    const int kr = n * (64 / KC) + lane / KC, vr = n * (64 / VC) + lane / VC;
+    const int kc = (lane % KC) ^ (kr & (KC - 1)), vc = (lane % VC) ^ (vr & (VC - 1));
+    koff[u] = (small ? kr & 31 : kr) * D + kc * 8;
+    voff[u] = vr * a.s.page + (small ? (vc & 3) * 8 : vc * 8);
+  }
+  const bool second = (lane % VC ^ (lane / VC & (VC - 1))) >= 4;   // the lane's V is of keys 32 ..
+  const int shift = 31 - __builtin_clz(a.s.page);
+  struct Pages { int a, b; };
+  auto pages_of = [&](int j) {
+    const int k = it.k0 + j * kStage, k2 = k + 32;
+    return Pages{clamp_page(a.s, scalar_word(table, k >> shift)),
+                 clamp_page(a.s, scalar_word(table, k2 >> shift))};
   };
-  u32x4 gk[LU], gv[LU];
-  auto load = [&](int j) {
-    if ((j & 31) == 0) {
-      const int k = min(it.k0 + j * 64 + lane * 32, it.k1 - 1);
-      ids = clamp_page(a.s, table[k / a.s.page]);
-    }
-    const size_t p0 = page_of(j, 0), p1 = page_of(j, 1);
-    const int k = it.k0 + j * 64;
+  auto in_page = [&](int j) { return small ? 0 : (it.k0 + j * kStage) & (a.s.page - 1); };
+  auto dma_k = [&](uint8_t* to, Pages pg, int j) {
 #pragma unroll
     for (int u = 0; u < LU; ++u) {
-      const int row = kr + u * (NT / KC);
-      gk[u] = *reinterpret_cast<const u32x4*>(kpool + (row < 32 ? p0 : p1) +
-                                              (size_t)((k + row) & (a.s.page - 1)) * D + kc * 8);
+      const int n = wave * LU + u;
+      const size_t id = n * (64 / KC) < 32 ? pg.a : pg.b;
+      const uint16_t* from = kpool + id * page_el + (size_t)in_page(j) * D;
+      __builtin_amdgcn_global_load_lds(LDR_GP(from + koff[u]), LDR_LP(to + n * 1024), 16, 0, 0);
     }
-    const uint16_t* vb = vpool + (vc < 4 ? p0 : p1) + ((k + vc * 8) & (a.s.page - 1));
+  };
+  auto dma_v = [&](uint8_t* to, Pages pg, int j) {
+    const uint16_t* a0 = vpool + pg.a * page_el + in_page(j);
+    const uint16_t* a1 = vpool + pg.b * page_el + in_page(j);
+    const uint16_t* from = second ? a1 : a0;
 #pragma unroll
     for (int u = 0; u < LU; ++u)
-      gv[u] = *reinterpret_cast<const u32x4*>(vb + (size_t)(vr + u * (NT / VC)) * a.s.page);
+      __builtin_amdgcn_global_load_lds(LDR_GP(from + voff[u]),
+                                       LDR_LP(to + (wave * LU + u) * 1024), 16, 0, 0);
   };
-  auto store = [&](int j) {
-    const int at = (j & 1) * STAGE;
-    if (j >= full) {
-      bool bad = false;
-#pragma unroll
-      for (int u = 0; u < LU; ++u)
-        bad = clean_values<uint16_t>(gv[u], it.k0 + j * 64 + vc * 8, it.k1) || bad;
-      if (bad) odd_values = 1;
-    }
-#pragma unroll
-    for (int u = 0; u < LU; ++u) {
-      const int row = kr + u * (NT / KC), vrow = vr + u * (NT / VC);
-      *reinterpret_cast<u32x4*>(sk + at + row * (2 * D) + ((kc ^ (row & (KC - 1))) << 4)) = gk[u];
-      *reinterpret_cast<u32x4*>(sv + at + vrow * 128 + ((vc ^ (vrow & (VC - 1))) << 4)) = gv[u];
-    }
+  auto buffer = [&](auto i) -> uint8_t* {
+    constexpr int I = decltype(i)::value & 3;
+    if constexpr (I == 0) return S0; else if constexpr (I == 1) return S1;
+    else if constexpr (I == 2) return S2; else return S3;
   };
+  Pages kp{0, 0}, vp{0, 0};   // of the next K, V to start
+  // barrier j, J = j mod 4
+  auto meet = [&](auto J, int j) {
+    wait_vmcnt<4 * LU>();
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    uint8_t* to = buffer(std::integral_constant<int, decltype(J)::value + 3>{});
+    dma_k(to, kp, min(j + 3, stages - 1));
+    dma_v(to + STAGE, vp, min(j + 2, stages - 1));
+    vp = kp;
+    kp = pages_of(min(j + 4, stages - 1));
+  };
+
   // fragments: K rows in the order that leaves a lane 8 consecutive keys. The
   // swizzle makes a fragment's offset that of the first with bits flipped.
   const int mi = ((col >> 3) << 2) | (col & 3), mh = (col >> 2) & 1;
   const int krow = mi / 8 * 16 + mh * 8 + mi % 8;
   const uint32_t klane = krow * (2 * D) + ((half ^ (krow & (KC - 1))) << 4);
   const uint32_t vlane = col * 128 + ((half ^ (col & (VC - 1))) << 4);
-  auto kfrag = [&](uint32_t at, int sub, int f) {
-    return *reinterpret_cast<const u32x4*>(sk + (klane ^ (at + (f << 5))) + sub * (64 * D));
-  };
-  auto vfrag = [&](uint32_t at, int dt, int f) {
-    return *reinterpret_cast<const u32x4*>(sv + (vlane ^ (at + (f << 5))) + dt * 4096);
-  };
 
   const float c2 = a.scale * 1.44269504088896341f;
   f32x16 o[ND] = {};
   float mu = -INFINITY, l = 0.f;
-  if (stages > 0) {
-    load(0);
-    store(0);
-    if (stages > 1) load(1);
-  }
-  for (int j = 0; j < stages; ++j) {
-    lds_barrier();   // stage j is whole, and stage j - 1 has been read
-    if (j + 1 < stages) store(j + 1);
-    if (j + 2 < stages) load(j + 2);
-    if (!active) continue;
-    const uint32_t at = (j & 1) * STAGE;
-    f32x16 sc[2] = {};
+  f32x16 sc[2];
+  u32x4 pf[4] = {};      // none before the first stage, and its V is 0
+  // The products of stage j, J = j mod 4: V^T P^T of j - 1, then (unless j is the
+  // end) K Q^T of j, two at a time, with the LDS reads kAhead fragments in front of
+  // them. The order is pinned: left to itself the compiler reads each fragment
+  // right before its product and waits for it. Half: 0 or 1, or both (2).
+  auto products = [&](auto scores, auto Half, auto J) {
+    constexpr int H = decltype(Half)::value, NS = H == 2 ? 2 : 1, F0 = H == 1 ? 2 : 0;
+    constexpr int G = 2, kAhead = 4, R = kAhead + G;
+    constexpr int NV = 2 * NS * ND, N = NV + (decltype(scores)::value ? NS * NF : 0);
+    static_assert(N % G == 0 && kAhead % G == 0, "whole groups");
+    const uint8_t* kb = buffer(J) + (H == 1 ? 64 * D : 0);
+    const uint8_t* vb = buffer(J) + STAGE;
+    u32x4 fr[R];
+    auto read = [&](int i) {
+      const int f = i < NV ? F0 + i / ND : (i - NV) / NS;
+      fr[i % R] = i < NV ? *reinterpret_cast<const u32x4*>(vb + (vlane ^ (f << 5)) + i % ND * 4096)
+                         : *reinterpret_cast<const u32x4*>(kb + (klane ^ (f << 5)) +
+                                                           (i - NV) % NS * (64 * D));
+    };
 #pragma unroll
-    for (int sub = 0; sub < 2; ++sub)
+    for (int i = 0; i < kAhead; ++i) read(i);
 #pragma unroll
-      for (int f = 0; f < NF; ++f) sc[sub] = M::run(kfrag(at, sub, f), qf[f], sc[sub]);
-    if (j >= full) {
-      const int lim = min(it.k1 - 1, last) - (it.k0 + j * 64);
+    for (int i0 = 0; i0 < N; i0 += G) {
+      __builtin_amdgcn_sched_barrier(0x6);
 #pragma unroll
-      for (int sub = 0; sub < 2; ++sub)
+      for (int i = i0 + kAhead; i < i0 + kAhead + G; ++i)
+        if (i < N) read(i);
+      __builtin_amdgcn_sched_barrier(0x6);
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (sub * 32 + i / 8 * 16 + half * 8 + i % 8 > lim) sc[sub][i] = -INFINITY;
+      for (int i = i0; i < i0 + G; ++i) {
+        if (i < NV) {
+          o[i % ND] = M::run(fr[i % R], pf[i / ND], o[i % ND]);
+        } else {
+          const int f = (i - NV) / NS, sub = (i - NV) % NS;
+          sc[sub] = M::run(fr[i % R], qf[f], f ? sc[sub] : f32x16{});
+        }
+      }
     }
-    float mx = fmaxf(sc[0][0], sc[1][0]);
+    __builtin_amdgcn_sched_barrier(0x6);
+  };
+  auto softmax = [&](auto Half) {
+    constexpr int NS = decltype(Half)::value == 2 ? 2 : 1;
+    float mx = sc[0][0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, fmaxf(sc[0][i], sc[1][i]));
+    for (int i = NS == 2 ? 0 : 1; i < 16; ++i)
+      mx = fmaxf(mx, NS == 2 ? fmaxf(sc[0][i], sc[1][i]) : sc[0][i]);
     mx = half_max(mx) * c2;
     const bool up = mx > mu + kLazy;
     if (__any(up)) {
@@ -705,10 +928,9 @@ attend_wide_kernel(AttendArgs a) {
       for (int dt = 0; dt < ND; ++dt) o[dt] *= alpha;
     }
     const float z = mu == -INFINITY ? 0.f : mu;
-    u32x4 pf[4];
     float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
+    for (int sub = 0; sub < NS; ++sub) {
       float x[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -719,115 +941,121 @@ attend_wide_kernel(AttendArgs a) {
       for (int f = 0; f < 2; ++f) pf[sub * 2 + f] = M::pack(x + 8 * f);
     }
     l += sum[0] + sum[1];
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-      for (int f = 0; f < 4; ++f) o[dt] = M::run(vfrag(at, dt, f), pf[f], o[dt]);
-  }
-  if (full < stages) {
-    lds_barrier();
-    if (odd_values)
-      for (int k = it.k0 + full * 64; k < it.k1; k += kKeys)
-        add_non_finite<uint16_t, ND>(o, vpool + clamp_page(a.s, table[k / a.s.page]) * page_el +
-                                            (k & (a.s.page - 1)),
-                                     a.s.page, min(kKeys, it.k1 - k), k, last, half);
-  }
+  };
 
-  // parts or results, straight from the registers
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  std::integral_constant<int, 0> i0;
+  std::integral_constant<int, 1> i1;
+  std::integral_constant<int, 2> i2;
+  std::integral_constant<int, 3> i3;
+  // K of stages 0 .. 2, V of 0 and 1, in the order in which the barriers wait
+  {
+    const Pages p0 = pages_of(0), p1 = pages_of(min(1, stages - 1));
+    vp = pages_of(min(2, stages - 1));
+    kp = pages_of(min(3, stages - 1));
+#pragma unroll
+    for (int u = 0; u < LU; ++u)
+      reinterpret_cast<u32x4*>(S0 + STAGE + (wave * LU + u) * 1024)[lane] = u32x4{};
+    __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));   // in LDS before barrier 0
+    dma_k(S0, p0, 0);
+    dma_k(S1, p1, min(1, stages - 1));
+    dma_v(S1 + STAGE, p0, 0);
+    dma_k(S2, vp, min(2, stages - 1));
+    dma_v(S2 + STAGE, p1, min(1, stages - 1));
+  }
+  // the stages of a wave without rows (its share of the loads, and the barriers),
+  // of the first group, or of the second
+  auto run = [&](auto works, auto late, auto Half) {
+    constexpr bool WORKS = decltype(works)::value, LATE = decltype(late)::value;
+    // slot j: a stage, behind the last one its values, then nothing but the barrier
+    auto slot = [&](auto J, int j) {
+      if constexpr (!LATE) meet(J, j);
+      if constexpr (WORKS) {
+        if (j < stages) {
+          __builtin_amdgcn_s_setprio(1);
+          products(yes, Half, J);
+          __builtin_amdgcn_s_setprio(0);
+        } else if (j == stages) {
+          products(no, Half, J);
+        }
+      }
+      if constexpr (LATE) meet(std::integral_constant<int, (decltype(J)::value + 1) & 3>{}, j + 1);
+      if constexpr (WORKS)
+        if (j < stages) softmax(Half);
+    };
+    if constexpr (LATE) meet(i0, 0);
+    for (int j = 0; j <= stages; j += 4) {
+      slot(i0, j);
+      slot(i1, j + 1);
+      slot(i2, j + 2);
+      slot(i3, j + 3);
+    }
+    if constexpr (!LATE) __builtin_amdgcn_s_barrier();   // as many as the other group's
+  };
+  if (!active) run(no, no, i2);
+  else if (wave < NW / 2) { if (split) run(yes, no, i0); else run(yes, no, i2); }
+  else { if (split) run(yes, yes, i1); else run(yes, yes, i2); }
+  wait_vmcnt<0>();   // no DMA outlives the workgroup
   l = half_sum(l);
-  const int row = wave * 32 + col;
-  if (row >= it.nr) return;
-  const float m = mu * 0.693147180559945309f;
-  if (it.part >= 0) {
-    const size_t pr = (size_t)head * a.w.part_rows + it.part + row;
-    float* out = reinterpret_cast<float*>(a.ws + a.w.o) + pr * D + half * 4;
+
+  if (split) {       // the second group's results reach the first through LDS
+    __syncthreads();
+    uint8_t* at = (block < 2 ? S0 : S1) + block % 2 * STAGE;
+    float4* po = reinterpret_cast<float4*>(at) + lane;
+    float2* ml = reinterpret_cast<float2*>(S2) + block * kBlock;
+    if (wave >= NW / 2) {
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
+      for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<float4*>(out + dt * 32 + g * 8) =
-            float4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
-    if (half == 0) reinterpret_cast<float2*>(a.ws + a.w.ml)[pr] = float2{m, l};
-  } else {
-    const int rr = it.r0 + row, q = rr / a.rep;
-    const size_t at = (size_t)map[it.q0 + q] * a.hq + head * a.rep + (rr - q * a.rep);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    uint16_t* out = static_cast<uint16_t*>(a.o) + at * D + half * 4;
+        for (int g = 0; g < 4; ++g)
+          po[(dt * 4 + g) * 64] = float4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2],
+                                         o[dt][4 * g + 3]};
+      if (half == 0) ml[col] = float2{mu, l};
+    }
+    __syncthreads();
+    if (wave >= NW / 2 || !active) return;
+    const float2 x = ml[col];
+    const float mn = fmaxf(mu, x.x), z = mn == -INFINITY ? 0.f : mn;
+    const float wo = __builtin_amdgcn_exp2f(mu - z), wx = __builtin_amdgcn_exp2f(x.x - z);
+    mu = mn;
+    l = l * wo + x.y * wx;
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        float x[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = o[dt][4 * g + k] * inv;
-        M::store4(out + dt * 32 + g * 8, x);
+        const float4 v = po[(dt * 4 + g) * 64];
+        o[dt][4 * g] = o[dt][4 * g] * wo + v.x * wx;
+        o[dt][4 * g + 1] = o[dt][4 * g + 1] * wo + v.y * wx;
+        o[dt][4 * g + 2] = o[dt][4 * g + 2] * wo + v.z * wx;
+        o[dt][4 * g + 3] = o[dt][4 * g + 3] * wo + v.w * wx;
       }
-    if (half == 0 && a.lse) a.lse[at] = l == 0.f ? -INFINITY : m + logf(l);
   }
-}
+  if (!active) return;
 
-// Joins the parts of each row: one wave per (row, query head).
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a) {
-  if (!plan_ok(a)) return;
-  const Header* hd = reinterpret_cast<const Header*>(a.ws);
-  const long id = (long)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  const int k = (int)(id / a.hq), h = (int)(id - (long)k * a.hq);
-  if (k >= hd->rows) return;
-  const int row = reinterpret_cast<const int32_t*>(a.ws + a.w.map)[k];
-  const SeqInfo f = reinterpret_cast<const SeqInfo*>(a.ws + a.w.info)[row / a.max_new];
-  if (f.own_part < 0) return;                 // finished by its only item
-  const int lane = threadIdx.x & 63, g = h / a.rep, hr = h - g * a.rep;
-  const int n = f.grp_chunks + f.own_chunks;
-  const long grp = f.grp_part + (long)(k - f.grp_qoff) * a.rep + hr;
-  const long own = f.own_part + (long)(k - f.qoff) * a.rep + hr;
-  const size_t base = (size_t)g * a.w.part_rows;
-  const float2* ml = reinterpret_cast<const float2*>(a.ws + a.w.ml) + base;
-  const float* po = reinterpret_cast<const float*>(a.ws + a.w.o) + base * D;
-  auto at = [&](int c) {
-    return c < f.grp_chunks ? grp + (long)c * f.grp_rows
-                            : own + (long)(c - f.grp_chunks) * f.own_rows;
-  };
-  float m = -INFINITY;
-  for (int c = lane; c < n; c += 64) m = fmaxf(m, ml[at(c)].x);
+  // the wave's block of partial results, straight from the registers
+  float4* out = reinterpret_cast<float4*>(part_o<D>(a, head, it.part + block)) + lane;
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
-  const float mu = m == -INFINITY ? 0.f : m;
-  constexpr int V = D / 64;
-  float acc[V] = {}, l = 0.f;
-  for (int c = 0; c < n; ++c) {
-    const long pr = at(c);
-    const float2 x = ml[pr];
-    const float wgt = __builtin_amdgcn_exp2f((x.x - mu) * 1.44269504088896341f);
-    l += x.y * wgt;
+  for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-    for (int v = 0; v < V; ++v) acc[v] += wgt * po[pr * D + lane * V + v];
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const size_t out = (size_t)row * a.hq + h;
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-    Elem<T>::store(static_cast<T*>(a.o) + out * D + lane * V + v, acc[v] * inv);
-  if (lane == 0 && a.lse) a.lse[out] = l == 0.f ? -INFINITY : m + logf(l);
+    for (int g = 0; g < 4; ++g)
+      out[(dt * 4 + g) * 64] = float4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2],
+                                      o[dt][4 * g + 3]};
+  if (half == 0) part_ml(a, head, it.part + block)[col] = float2{mu / c2, l};
 }
 
 template <typename T, int D>
 hipError_t launch(const AttendArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((attend_kernel<T, D>), dim3((unsigned)a.w.max_items * a.s.hkv),
-                     dim3(kThreads), 0, st, a);
+  const dim3 grid((unsigned)a.w.max_items * a.s.hkv);
+  if constexpr (sizeof(T) == 2)
+    hipLaunchKernelGGL(attend_wide_kernel<D>, grid, dim3(kWideThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((attend_rows_kernel<T, D, false>), grid, dim3(kThreads), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if constexpr (sizeof(T) == 2) {
-    if (a.w.max_wide > 0) {
-      hipLaunchKernelGGL(attend_wide_kernel<D>, dim3((unsigned)a.w.max_wide * a.s.hkv),
-                         dim3(kWideThreads), 0, st, a);
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
-    }
-  }
-  const long rows = (long)a.s.batch * a.max_new * a.hq;
-  hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)((rows + 3) / 4)), dim3(kThreads),
-                     0, st, a);
+  hipLaunchKernelGGL((attend_rows_kernel<T, D, true>),
+                     dim3((unsigned)((long)a.s.batch * a.w.tiles * a.s.hkv)), dim3(kThreads), 0,
+                     st, a);
   return hipGetLastError();
 }
 
