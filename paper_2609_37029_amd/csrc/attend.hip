@@ -451,8 +451,8 @@ __device__ inline float half_sum(float x) { return x + other_half(x); }
 
 // V where a mask crosses a step: keys from k1 on hold anything and count as 0. A
 // value that is not finite but masked for some rows only would reach them as
-// 0 x inf: it is taken out here (true: there was one), and add_non_finite adds
-// it to the rows that see it. `k`: the key of the fragment's first element.
+// 0 x inf: it is taken out here (true: there was one), to be added to the rows
+// that see it when they are written. `k`: the key of the fragment's first element.
 template <typename T> __device__ inline bool clean_values(u32x4& v, int k, int k1) {
   constexpr int E = Mma<T>::E;
 #pragma unroll
@@ -470,20 +470,6 @@ template <typename T> __device__ inline bool clean_values(u32x4& v, int k, int k
     else v[j] = inf ? 0u : v[j];
   }
   return bad;
-}
-// vt: the V^T rows of a head, at the first of n keys, the first of which is k.
-template <typename T, int ND>
-__device__ inline void add_non_finite(f32x16 (&o)[ND], const T* vt, int page, int n, int k, int last,
-                                      int half) {
-  for (int j = 0; j < n && k + j <= last; ++j)
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int dim = dt * 32 + i / 4 * 8 + half * 4 + i % 4;
-        const float v = Elem<T>::load(vt + (size_t)dim * page + j);
-        if (!(fabsf(v) < INFINITY)) o[dt][i] += v;
-      }
 }
 
 // A block's partial results: O^T as the matrix products leave it, 16 bytes a lane
@@ -507,7 +493,8 @@ __device__ inline float2* part_ml(const AttendArgs& a, int head, long block) {
 // parts in turn, and the results are written. Else: an item of the f32 main
 // kernel, its results a part.
 template <typename T, int D, bool FINISH>
-__global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) * D <= 256 ? 2 : 1)
+attend_rows_kernel(AttendArgs a) {
   using M = Mma<T>;
   constexpr int E = M::E, NF = D / (2 * E), ND = D / 32, NP = 16 / E, W = kThreads / 64;
   const int unit = (int)(blockIdx.x / a.s.hkv), head = (int)(blockIdx.x % a.s.hkv);
@@ -553,6 +540,7 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
   const float c2 = a.scale * 1.44269504088896341f;
   f32x16 o[ND] = {};
   float m = -INFINITY, l = 0.f;
+  bool bad = false;   // V held a value that is not finite where a mask is
 
   const int steps = (max(it.k1 - it.k0, 0) + kStep - 1) / kStep;
   int ids = 0;    // the pages of this wave's next 64 steps, one a lane
@@ -574,46 +562,33 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
   };
   if (wave < steps) fetch(0);
   if constexpr (FINISH) {
-    // parts: the group's chunks, then the tile's own; two at a time
+    // parts: the group's chunks, then the tile's own
     const int t = it.r0 / tile_of(a.s).rows * tile_of(a.s).rows;
     const int own = f.own_chunks
                         ? (tile_keys(f.rows, f.open, f.share, t, a.rep) + f.step - 1) / f.step : 0;
-    const int gr = f.grp_off + r, parts = f.grp_chunks + own;
-    constexpr int U = 2;
-    for (int c0 = wave; c0 < parts; c0 += W * U) {
-      float2 ml[U];
-      const float4* po[U];
-      float4 v[U][D / 8];
+    const int gr = f.grp_off + r;
+    for (int c = wave; c < f.grp_chunks + own; c += W) {
+      const bool g = c < f.grp_chunks;
+      const long block = g ? f.grp_part + (long)c * f.grp_blocks + gr / kBlock
+                           : f.own_part + (long)(c - f.grp_chunks) * f.own_blocks + it.r0 / kBlock;
+      const int at = g ? gr % kBlock : r % kBlock;
+      const float2 ml = part_ml(a, head, block)[at];
+      const float4* po = reinterpret_cast<const float4*>(part_o<D>(a, head, block)) + half * 32 + at;
+      float4 v[D / 8];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int c = c0 + u * W < parts ? c0 + u * W : c0;
-        const bool g = c < f.grp_chunks;
-        const long block = g ? f.grp_part + (long)c * f.grp_blocks + gr / kBlock
-                             : f.own_part + (long)(c - f.grp_chunks) * f.own_blocks + it.r0 / kBlock;
-        const int at = g ? gr % kBlock : r % kBlock;
-        ml[u] = part_ml(a, head, block)[at];
-        if (c0 + u * W >= parts) ml[u] = float2{-INFINITY, 0.f};
-        po[u] = reinterpret_cast<const float4*>(part_o<D>(a, head, block)) + half * 32 + at;
+      for (int i = 0; i < D / 8; ++i) v[i] = po[i * 64];
+      const float mn = fmaxf(m, ml.x), mu = mn == -INFINITY ? 0.f : mn;
+      const float wo = __builtin_amdgcn_exp2f((m - mu) * c2);
+      const float wp = __builtin_amdgcn_exp2f((ml.x - mu) * c2);
+      m = mn;
+      l = l * wo + ml.y * wp;
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) v[u][i] = po[u][i * 64];
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const float mn = fmaxf(m, ml[u].x), mu = mn == -INFINITY ? 0.f : mn;
-        const float wo = __builtin_amdgcn_exp2f((m - mu) * c2);
-        const float wp = __builtin_amdgcn_exp2f((ml[u].x - mu) * c2);
-        const bool none = ml[u].y == 0.f;      // nothing, or a part that is not there
-        m = mn;
-        l = l * wo + ml[u].y * wp;
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          const float4 x = none ? float4{} : v[u][i];
-          const int dt = i / 4, q = i % 4 * 4;
-          o[dt][q] = o[dt][q] * wo + x.x * wp;
-          o[dt][q + 1] = o[dt][q + 1] * wo + x.y * wp;
-          o[dt][q + 2] = o[dt][q + 2] * wo + x.z * wp;
-          o[dt][q + 3] = o[dt][q + 3] * wo + x.w * wp;
-        }
+      for (int i = 0; i < D / 8; ++i) {
+        const int dt = i / 4, q = i % 4 * 4;
+        o[dt][q] = o[dt][q] * wo + v[i].x * wp;
+        o[dt][q + 1] = o[dt][q + 1] * wo + v[i].y * wp;
+        o[dt][q + 2] = o[dt][q + 2] * wo + v[i].z * wp;
+        o[dt][q + 3] = o[dt][q + 3] * wo + v[i].w * wp;
       }
     }
     l = half ? 0.f : l;      // of both halves; the steps' sums are of one each
@@ -659,20 +634,12 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
     u32x4 pf[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) pf[i] = M::pack(x + i * E);
-    if (FINISH && kb + kStep > cbase + it.r0 / a.rep + 1) {
-      bool bad = false;
+    if (FINISH && kb + kStep > cbase + it.r0 / a.rep + 1)
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
         for (int i = 0; i < NP; ++i)
           bad = clean_values<T>(vf[dt][i], kb + i * 2 * E + half * E, it.k1) || bad;
-      if (__any(bad)) {
-        const size_t off = (size_t)clamp_page(a.s, table[kb / a.s.page]) * a.s.page_bytes;
-        add_non_finite<T, ND>(o, reinterpret_cast<const T*>(vpool + off) + hoff +
-                                     (kb & (a.s.page - 1)),
-                              a.s.page, min(kStep, it.k1 - kb), kb, cbase + qi, half);
-      }
-    }
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
@@ -683,6 +650,9 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
   // join the waves: each one's (m, l) of the 32 rows, then O scaled to the common
   // maximum and added up, four values a thread
   __shared__ float sm[W][32], sl[W][32];
+  __shared__ int odd[W];
+  const bool any_bad = __any(bad);
+  if (lane == 0) odd[wave] = any_bad;
   constexpr int LD = D + 4;
   __shared__ alignas(16) float so[W][32 * LD];
   if (half == 0) { sm[wave][col] = m; sl[wave][col] = l; }
@@ -721,6 +691,19 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
       const float inv = ll == 0.f ? 0.f : 1.f / ll;
 #pragma unroll
       for (int k = 0; k < 4; ++k) acc[k] *= inv;
+      if (odd[0] | odd[1] | odd[2] | odd[3]) {   // what clean_values took out
+        const int s0 = max(0, cbase + it.r0 / a.rep + 1 - it.k0) / kStep;
+        for (int k = it.k0 + s0 * kStep; k <= cbase + q; ++k) {
+          const T* vt = reinterpret_cast<const T*>(
+                            vpool + (size_t)clamp_page(a.s, table[k / a.s.page]) * a.s.page_bytes) +
+                        hoff + (k & (a.s.page - 1));
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const float v = Elem<T>::load(vt + (size_t)(e + d) * a.s.page);
+            if (!(fabsf(v) < INFINITY)) acc[d] += v;
+          }
+        }
+      }
       M::store4(static_cast<T*>(a.o) + at * D + e, acc);
       if (e == 0 && a.lse) a.lse[at] = ll == 0.f ? -INFINITY : mm * a.scale + logf(ll);
     } else {
