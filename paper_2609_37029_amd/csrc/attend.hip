@@ -735,13 +735,19 @@ attend_rows_kernel(AttendArgs a) {
 // barriers j and j + 1. What was read before barrier j (the buffer of j - 1) is
 // filled again right behind it, for stage j + 3; a wave waits for its share of
 // buffer j in front of barrier j. Separate arrays let the compiler see that a
-// read does not depend on the DMA in flight. A 16-byte chunk c of row r lies at
-// chunk c ^ (r mod chunks a row): reads of 32 rows spread over the banks.
+// read does not depend on the DMA in flight. Rows are turned (below), so that the
+// reads of 16 of them spread over the banks.
 constexpr float kLazy = 8.f;
 
 template <int N> __device__ inline void wait_vmcnt() {
   static_assert(N >= 0 && N < 64, "vmcnt");
   __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+// The chunk of row r lies at its own number with these bits flipped, rows of C
+// chunks: 16 rows then have 16 places mod 256 bytes.
+template <int C> __device__ inline int turn(int r) {
+  static_assert(C == 16 || C == 8, "rows of 256 or 128 bytes");
+  return C == 16 ? r & 15 : (r >> 1) & 7;
 }
 #define LDR_GP(p) ((__attribute__((address_space(1))) void*)(p))
 #define LDR_LP(p) ((__attribute__((address_space(3))) void*)(p))
@@ -787,49 +793,63 @@ attend_wide_kernel(AttendArgs a) {
 
   // DMA. A half stage starts a page of 32, a stage lies at a multiple of 64 of a
   // larger one: the lanes' offsets in it stay.
-  const bool small = a.s.page == 32;
+  const int shift = 31 - __builtin_clz(a.s.page);
+  const bool small = shift == 5;
   uint32_t koff[LU], voff[LU];
+  bool second[LU];     // the lane's V is of keys 32 ..
 #pragma unroll
   for (int u = 0; u < LU; ++u) {
     const int n = wave * LU + u;
     const int kr = n * (64 / KC) + lane / KC, vr = n * (64 / VC) + lane / VC;
-    const int kc = (lane % KC) ^ (kr & (KC - 1)), vc = (lane % VC) ^ (vr & (VC - 1));
-    koff[u] = (small ? kr & 31 : kr) * D + kc * 8;
-    voff[u] = vr * a.s.page + (small ? (vc & 3) * 8 : vc * 8);
+    const int kc = (lane % KC) ^ turn<KC>(kr), vc = (lane % VC) ^ turn<VC>(vr);
+    koff[u] = ((small ? kr & 31 : kr) * D + kc * 8) * 2;
+    voff[u] = (vr * a.s.page + (small ? (vc & 3) * 8 : vc * 8)) * 2;
+    second[u] = vc >= 4;
   }
-  const bool second = (lane % VC ^ (lane / VC & (VC - 1))) >= 4;   // the lane's V is of keys 32 ..
-  const int shift = 31 - __builtin_clz(a.s.page);
-  struct Pages { int a, b; };
-  auto pages_of = [&](int j) {
-    const int k = it.k0 + j * kStage, k2 = k + 32;
-    return Pages{clamp_page(a.s, scalar_word(table, k >> shift)),
-                 clamp_page(a.s, scalar_word(table, k2 >> shift))};
+  // where a stage's keys are: elements from the pool's start to its page (and, of
+  // pages of 32, that of its second half), keys into it
+  struct Place { size_t a, b; int in; };
+  struct Ids { int a, b; };
+  auto ids_of = [&](int j) {     // on their way until they are looked at
+    const int k = it.k0 + j * kStage;
+    return Ids{scalar_word(table, k >> shift), small ? scalar_word(table, (k + 32) >> shift) : 0};
   };
-  auto in_page = [&](int j) { return small ? 0 : (it.k0 + j * kStage) & (a.s.page - 1); };
-  auto dma_k = [&](uint8_t* to, Pages pg, int j) {
+  auto place = [&](Ids ids, int j) {
+    Place p;
+    p.a = (size_t)clamp_page(a.s, ids.a) * page_el;
+    p.b = small ? (size_t)clamp_page(a.s, ids.b) * page_el : p.a;
+    p.in = small ? 0 : (it.k0 + j * kStage) & (a.s.page - 1);
+    return p;
+  };
+  auto dma_k = [&](uint8_t* to, const Place& p) {
 #pragma unroll
     for (int u = 0; u < LU; ++u) {
       const int n = wave * LU + u;
-      const size_t id = n * (64 / KC) < 32 ? pg.a : pg.b;
-      const uint16_t* from = kpool + id * page_el + (size_t)in_page(j) * D;
+      const uint8_t* from =
+          reinterpret_cast<const uint8_t*>(kpool + (n * (64 / KC) < 32 ? p.a : p.b) + p.in * D);
       __builtin_amdgcn_global_load_lds(LDR_GP(from + koff[u]), LDR_LP(to + n * 1024), 16, 0, 0);
     }
   };
-  auto dma_v = [&](uint8_t* to, Pages pg, int j) {
-    const uint16_t* a0 = vpool + pg.a * page_el + in_page(j);
-    const uint16_t* a1 = vpool + pg.b * page_el + in_page(j);
-    const uint16_t* from = second ? a1 : a0;
+  auto dma_v = [&](uint8_t* to, const Place& p) {
+    const uint8_t* from = reinterpret_cast<const uint8_t*>(vpool + p.a + p.in);
+    const size_t apart = (p.b - p.a) * 2;
 #pragma unroll
-    for (int u = 0; u < LU; ++u)
-      __builtin_amdgcn_global_load_lds(LDR_GP(from + voff[u]),
-                                       LDR_LP(to + (wave * LU + u) * 1024), 16, 0, 0);
+    for (int u = 0; u < LU; ++u) {
+      uint8_t* at = to + (wave * LU + u) * 1024;
+      if (small)
+        __builtin_amdgcn_global_load_lds(LDR_GP(from + (second[u] ? apart : 0) + voff[u]),
+                                         LDR_LP(at), 16, 0, 0);
+      else
+        __builtin_amdgcn_global_load_lds(LDR_GP(from + voff[u]), LDR_LP(at), 16, 0, 0);
+    }
   };
   auto buffer = [&](auto i) -> uint8_t* {
     constexpr int I = decltype(i)::value & 3;
     if constexpr (I == 0) return S0; else if constexpr (I == 1) return S1;
     else if constexpr (I == 2) return S2; else return S3;
   };
-  Pages kp{0, 0}, vp{0, 0};   // of the next K, V to start
+  Ids next;       // pages of the next K to start
+  Place vp;       // and where the next V is
   // barrier j, J = j mod 4
   auto meet = [&](auto J, int j) {
     wait_vmcnt<4 * LU>();
@@ -837,18 +857,19 @@ attend_wide_kernel(AttendArgs a) {
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
     uint8_t* to = buffer(std::integral_constant<int, decltype(J)::value + 3>{});
-    dma_k(to, kp, min(j + 3, stages - 1));
-    dma_v(to + STAGE, vp, min(j + 2, stages - 1));
+    const Place kp = place(next, min(j + 3, stages - 1));
+    next = ids_of(min(j + 4, stages - 1));
+    dma_k(to, kp);
+    dma_v(to + STAGE, vp);
     vp = kp;
-    kp = pages_of(min(j + 4, stages - 1));
   };
 
   // fragments: K rows in the order that leaves a lane 8 consecutive keys. The
   // swizzle makes a fragment's offset that of the first with bits flipped.
   const int mi = ((col >> 3) << 2) | (col & 3), mh = (col >> 2) & 1;
   const int krow = mi / 8 * 16 + mh * 8 + mi % 8;
-  const uint32_t klane = krow * (2 * D) + ((half ^ (krow & (KC - 1))) << 4);
-  const uint32_t vlane = col * 128 + ((half ^ (col & (VC - 1))) << 4);
+  const uint32_t klane = krow * (2 * D) + ((half ^ turn<KC>(krow)) << 4);
+  const uint32_t vlane = col * 128 + ((half ^ turn<VC>(col)) << 4);
 
   const float c2 = a.scale * 1.44269504088896341f;
   f32x16 o[ND] = {};
@@ -934,47 +955,60 @@ attend_wide_kernel(AttendArgs a) {
   std::integral_constant<int, 3> i3;
   // K of stages 0 .. 2, V of 0 and 1, in the order in which the barriers wait
   {
-    const Pages p0 = pages_of(0), p1 = pages_of(min(1, stages - 1));
-    vp = pages_of(min(2, stages - 1));
-    kp = pages_of(min(3, stages - 1));
+    const int j1 = min(1, stages - 1), j2 = min(2, stages - 1);
+    const Ids n0 = ids_of(0), n1 = ids_of(j1), n2 = ids_of(j2);
+    next = ids_of(min(3, stages - 1));
+    const Place p0 = place(n0, 0), p1 = place(n1, j1);
+    vp = place(n2, j2);
 #pragma unroll
     for (int u = 0; u < LU; ++u)
       reinterpret_cast<u32x4*>(S0 + STAGE + (wave * LU + u) * 1024)[lane] = u32x4{};
     __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));   // in LDS before barrier 0
-    dma_k(S0, p0, 0);
-    dma_k(S1, p1, min(1, stages - 1));
-    dma_v(S1 + STAGE, p0, 0);
-    dma_k(S2, vp, min(2, stages - 1));
-    dma_v(S2 + STAGE, p1, min(1, stages - 1));
+    dma_k(S0, p0);
+    dma_k(S1, p1);
+    dma_v(S1 + STAGE, p0);
+    dma_k(S2, vp);
+    dma_v(S2 + STAGE, p1);
   }
   // the stages of a wave without rows (its share of the loads, and the barriers),
   // of the first group, or of the second
   auto run = [&](auto works, auto late, auto Half) {
     constexpr bool WORKS = decltype(works)::value, LATE = decltype(late)::value;
-    // slot j: a stage, behind the last one its values, then nothing but the barrier
+    // slot j: a stage, or behind the last one nothing but the barrier and its DMA
+    // (which then brings the last stage again, to where it is or nobody reads)
     auto slot = [&](auto J, int j) {
       if constexpr (!LATE) meet(J, j);
-      if constexpr (WORKS) {
+      if constexpr (WORKS)
         if (j < stages) {
           __builtin_amdgcn_s_setprio(1);
           products(yes, Half, J);
           __builtin_amdgcn_s_setprio(0);
-        } else if (j == stages) {
-          products(no, Half, J);
         }
-      }
       if constexpr (LATE) meet(std::integral_constant<int, (decltype(J)::value + 1) & 3>{}, j + 1);
       if constexpr (WORKS)
         if (j < stages) softmax(Half);
     };
     if constexpr (LATE) meet(i0, 0);
-    for (int j = 0; j <= stages; j += 4) {
+    for (int j = 0; j < stages; j += 4) {
       slot(i0, j);
       slot(i1, j + 1);
       slot(i2, j + 2);
       slot(i3, j + 3);
     }
-    if constexpr (!LATE) __builtin_amdgcn_s_barrier();   // as many as the other group's
+    if constexpr (!LATE) {   // as many barriers as the other group's
+      wait_vmcnt<0>();
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (WORKS) {   // the last stage's values
+      switch (stages & 3) {
+        case 0: products(no, Half, i0); break;
+        case 1: products(no, Half, i1); break;
+        case 2: products(no, Half, i2); break;
+        default: products(no, Half, i3);
+      }
+    }
   };
   if (!active) run(no, no, i2);
   else if (wave < NW / 2) { if (split) run(yes, no, i0); else run(yes, no, i2); }
