@@ -8,10 +8,10 @@
 // share, and the rows of each sequence over its own keys. A segment is cut into
 // tiles of rows and chunks of keys, enough items to fill the GPU. A plan kernel
 // writes the list of items (the lengths are on the device), one workgroup of the
-// main kernel takes an item of one K/V head. Items hold whole stages of 64 keys
-// that all rows of their tile see; the keys behind them, where the mask runs
-// (fewer than 128 a tile, or all where they are few), go to the last kernel, which
-// also joins the parts of its rows.
+// main kernel takes an item of one K/V head. Items hold whole units of 256 keys
+// (128 of fp32) that all rows of their tile see; the keys behind them, where the
+// mask runs (or all of a sequence's own where they are few), go to the last kernel,
+// which also joins the parts of its rows.
 #include <type_traits>
 
 #include "ldr_internal.h"
@@ -27,17 +27,18 @@ constexpr int kThreads = 256;
 constexpr int kWideThreads = 512;
 constexpr int kBook = 1024;          // threads of the plan's workgroup
 constexpr int kStep = 32;            // keys of a step; a page holds whole steps
-constexpr int kStage = 64;           // keys of a stage: an item's keys are whole ones
-constexpr int kMinShared = 128;      // keys in common that are worth a segment of their own
+constexpr int kStage = 64;           // keys of a stage of the bf16 main kernel
+constexpr int kMinShared = 256;      // keys in common that are worth a segment of their own
 constexpr int kMinMain = 512;        // keys of a sequence's own that are worth items
 constexpr int kBlock = 32;           // rows of a block of partial results
 
-// Tiles of a dtype's main kernel: rows of an item, workgroups that run at once,
-// and the keys whose work an item costs on top of its own (its start, and writing
-// and joining its part).
-struct Tile { int rows, slots, cost; };
+// Tiles of a dtype's main kernel: rows of an item, the keys that an item's are a
+// multiple of (four stages: the bf16 kernel's loop has no branch), workgroups that
+// run at once, and the keys whose work an item costs on top of its own (its start,
+// and writing and joining its part).
+struct Tile { int rows, unit, slots, cost; };
 __host__ __device__ inline Tile tile_of(const PagesShape& s) {
-  return s.dtype == LDR_BF16 ? Tile{256, 256, 384} : Tile{32, 512, 192};
+  return s.dtype == LDR_BF16 ? Tile{256, 4 * kStage, 256, 384} : Tile{32, 128, 512, 192};
 }
 // Rounds of items over the workgroups that run at once, at most.
 constexpr int kMaxRounds = 4;
@@ -59,9 +60,9 @@ struct SeqInfo {
 static_assert(sizeof(Item) == 32 && sizeof(SeqInfo) == 64, "read as words");
 
 // Keys, from `share` on, that every row of the tile from row t on sees and items
-// can take: whole stages.
-__device__ inline int tile_keys(int rows, int open, int share, int t, int rep) {
-  return max(0, rows - open + t / rep + 1 - share) / kStage * kStage;
+// can take: whole units.
+__device__ inline int tile_keys(int rows, int open, int share, int t, int rep, int unit) {
+  return max(0, rows - open + t / rep + 1 - share) / unit * unit;
 }
 
 struct Header { int version, hq, max_new, items, pad[60]; };
@@ -135,9 +136,9 @@ __device__ inline int wave_sum(int v) {
   return v;
 }
 
-// Keys of each of n even chunks of len: whole stages.
-__device__ inline int even_step(int len, int n) {
-  return ((len + n - 1) / n + kStage - 1) / kStage * kStage;
+// Keys of each of n even chunks of len: whole units.
+__device__ inline int even_step(int len, int n, int unit) {
+  return ((len + n - 1) / n + unit - 1) / unit * unit;
 }
 
 // The plan, in one workgroup: thread b has sequence b; what looks at all
@@ -234,12 +235,12 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   // segments: a sequence's own rows over its own keys; a group's rows, kept with
   // its first sequence, over the shared ones
   const int ld = in ? lead[b] : b;
-  const int common_rows = in ? common[ld] * s.page / kStage * kStage : 0;
+  const int common_rows = in ? common[ld] * s.page / tile.unit * tile.unit : 0;
   const int share = in && members[b] > 1 && common_rows >= kMinShared ? common_rows : 0;
   const int gopen = in ? gopens[b] : 0;
   const long R = (long)open * rep, Rg = share && ld == b ? (long)gopen * rep : 0;
   const int ot = (int)ceil_div(R, tile.rows), gt = (int)ceil_div(Rg, tile.rows);
-  int len = open ? tile_keys(rows, open, share, (ot - 1) * tile.rows, rep) : 0;
+  int len = open ? tile_keys(rows, open, share, (ot - 1) * tile.rows, rep, tile.unit) : 0;
   if (len < kMinMain) len = 0;
   const int glen = Rg ? share : 0;
   o_len[b] = len;
@@ -251,13 +252,13 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   // a chunk's; else it is near an even spread, and half a chunk at the end.
   {
     const float even = (float)work * s.hkv / tile.slots;
-    const int least = max((int)min(even / kMaxRounds + 1.f, 5e8f), kStage);
+    const int least = max((int)min(even / kMaxRounds + 1.f, 5e8f), tile.unit);
     float best = INFINITY;
     int chunk = 0;
     for (int t = wave; t < 4 * NW; t += NW) {
       // from `least` to 2 x kMaxRounds of it, in even ratios
       const float x = least * __builtin_amdgcn_exp2f(t * (3.2f / (4 * NW)));
-      const int c = (int)ceil_div((long)x, kStage) * kStage;
+      const int c = (int)ceil_div((long)x, tile.unit) * tile.unit;
       int n = 0;
       for (int i = lane; i < s.batch; i += 64) {
         const int l = o_len[i], o = opens[i];
@@ -298,7 +299,7 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
     f.open = open;
     f.rows = rows;
     f.share = share;
-    f.step = oc ? even_step(len, oc) : kStage;
+    f.step = oc ? even_step(len, oc, tile.unit) : tile.unit;
     f.own_part = o_part[b];
     f.own_chunks = oc;
     f.own_blocks = ob;
@@ -334,8 +335,9 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
     const int tiles = (n + tile.rows - 1) / tile.rows;
     const int c = k / tiles, r0 = (k - c * tiles) * tile.rows;
     const int from = g ? 0 : shares[lo];
-    const int keys = g ? shares[lo] : tile_keys(ends[lo], opens[lo], from, r0, rep);
-    const int step = even_step(g ? shares[lo] : o_len[lo], g ? g_chunks[lo] : o_chunks[lo]);
+    const int keys = g ? shares[lo] : tile_keys(ends[lo], opens[lo], from, r0, rep, tile.unit);
+    const int step = even_step(g ? shares[lo] : o_len[lo], g ? g_chunks[lo] : o_chunks[lo],
+                               tile.unit);
     Item it;
     it.q0 = qoffs[lo];
     it.r0 = r0;
@@ -511,7 +513,7 @@ attend_rows_kernel(AttendArgs a) {
     it.q0 = f.qoff;
     cbase = f.rows - f.open;
     const int t = it.r0 / tile_of(a.s).rows * tile_of(a.s).rows;
-    it.k0 = f.share + (f.own_chunks ? tile_keys(f.rows, f.open, f.share, t, a.rep) : 0);
+    it.k0 = f.share + (f.own_chunks ? tile_keys(f.rows, f.open, f.share, t, a.rep, tile_of(a.s).unit) : 0);
     it.k1 = cbase + (it.r0 + it.nr - 1) / a.rep + 1;
   } else {
     it = scalar_item(a.ws + a.w.items, unit);
@@ -565,7 +567,7 @@ attend_rows_kernel(AttendArgs a) {
     // parts: the group's chunks, then the tile's own
     const int t = it.r0 / tile_of(a.s).rows * tile_of(a.s).rows;
     const int own = f.own_chunks
-                        ? (tile_keys(f.rows, f.open, f.share, t, a.rep) + f.step - 1) / f.step : 0;
+                        ? (tile_keys(f.rows, f.open, f.share, t, a.rep, tile_of(a.s).unit) + f.step - 1) / f.step : 0;
     const int gr = f.grp_off + r;
     for (int c = wave; c < f.grp_chunks + own; c += W) {
       const bool g = c < f.grp_chunks;
@@ -733,8 +735,8 @@ attend_rows_kernel(AttendArgs a) {
 // K and V^T go to LDS by DMA, three stages ahead, in a ring of four buffers: the
 // one of stage j has K of j and V of j - 1, which its products read between
 // barriers j and j + 1. What was read before barrier j (the buffer of j - 1) is
-// filled again right behind it, for stage j + 3; a wave waits for its share of
-// buffer j in front of barrier j. Separate arrays let the compiler see that a
+// filled again among those products, for stage j + 3; a wave waits for its share
+// of buffer j in front of barrier j. Separate arrays let the compiler see that a
 // read does not depend on the DMA in flight. Rows are turned (below), so that the
 // reads of 16 of them spread over the banks.
 constexpr float kLazy = 8.f;
@@ -821,27 +823,17 @@ attend_wide_kernel(AttendArgs a) {
     p.in = small ? 0 : (it.k0 + j * kStage) & (a.s.page - 1);
     return p;
   };
-  auto dma_k = [&](uint8_t* to, const Place& p) {
-#pragma unroll
-    for (int u = 0; u < LU; ++u) {
-      const int n = wave * LU + u;
-      const uint8_t* from =
-          reinterpret_cast<const uint8_t*>(kpool + (n * (64 / KC) < 32 ? p.a : p.b) + p.in * D);
-      __builtin_amdgcn_global_load_lds(LDR_GP(from + koff[u]), LDR_LP(to + n * 1024), 16, 0, 0);
-    }
+  auto dma_k = [&](uint8_t* to, const Place& p, int u) {
+    const int n = wave * LU + u;
+    const uint8_t* from =
+        reinterpret_cast<const uint8_t*>(kpool + (n * (64 / KC) < 32 ? p.a : p.b) + p.in * D);
+    __builtin_amdgcn_global_load_lds(LDR_GP(from + koff[u]), LDR_LP(to + n * 1024), 16, 0, 0);
   };
-  auto dma_v = [&](uint8_t* to, const Place& p) {
+  auto dma_v = [&](uint8_t* to, const Place& p, int u) {
     const uint8_t* from = reinterpret_cast<const uint8_t*>(vpool + p.a + p.in);
-    const size_t apart = (p.b - p.a) * 2;
-#pragma unroll
-    for (int u = 0; u < LU; ++u) {
-      uint8_t* at = to + (wave * LU + u) * 1024;
-      if (small)
-        __builtin_amdgcn_global_load_lds(LDR_GP(from + (second[u] ? apart : 0) + voff[u]),
-                                         LDR_LP(at), 16, 0, 0);
-      else
-        __builtin_amdgcn_global_load_lds(LDR_GP(from + voff[u]), LDR_LP(at), 16, 0, 0);
-    }
+    const size_t apart = small && second[u] ? (p.b - p.a) * 2 : 0;
+    __builtin_amdgcn_global_load_lds(LDR_GP(from + apart + voff[u]),
+                                     LDR_LP(to + (wave * LU + u) * 1024), 16, 0, 0);
   };
   auto buffer = [&](auto i) -> uint8_t* {
     constexpr int I = decltype(i)::value & 3;
@@ -849,19 +841,22 @@ attend_wide_kernel(AttendArgs a) {
     else if constexpr (I == 2) return S2; else return S3;
   };
   Ids next;       // pages of the next K to start
-  Place vp;       // and where the next V is
+  Place kp, vp;   // where the K and V to start behind the last barrier are
   // barrier j, J = j mod 4
-  auto meet = [&](auto J, int j) {
+  auto meet = [&](int j) {
     wait_vmcnt<4 * LU>();
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    uint8_t* to = buffer(std::integral_constant<int, decltype(J)::value + 3>{});
-    const Place kp = place(next, min(j + 3, stages - 1));
-    next = ids_of(min(j + 4, stages - 1));
-    dma_k(to, kp);
-    dma_v(to + STAGE, vp);
     vp = kp;
+    kp = place(next, min(j + 3, stages - 1));
+    next = ids_of(min(j + 4, stages - 1));
+  };
+  // the DMA behind barrier j, one instruction of 2 LU
+  auto start = [&](auto J, int q) {
+    uint8_t* to = buffer(std::integral_constant<int, decltype(J)::value + 3>{});
+    if (q < LU) dma_k(to, kp, q);
+    else dma_v(to + STAGE, vp, q - LU);
   };
 
   // fragments: K rows in the order that leaves a lane 8 consecutive keys. The
@@ -899,6 +894,8 @@ attend_wide_kernel(AttendArgs a) {
 #pragma unroll
     for (int i0 = 0; i0 < N; i0 += G) {
       __builtin_amdgcn_sched_barrier(0x6);
+      // the DMA in between, one at a time: 4 of each wave at once stall them all
+      if (decltype(scores)::value && i0 % (N / (2 * LU)) == 0) start(J, i0 / (N / (2 * LU)));
 #pragma unroll
       for (int i = i0 + kAhead; i < i0 + kAhead + G; ++i)
         if (i < N) read(i);
@@ -959,56 +956,44 @@ attend_wide_kernel(AttendArgs a) {
     const Ids n0 = ids_of(0), n1 = ids_of(j1), n2 = ids_of(j2);
     next = ids_of(min(3, stages - 1));
     const Place p0 = place(n0, 0), p1 = place(n1, j1);
-    vp = place(n2, j2);
+    kp = place(n2, j2);
 #pragma unroll
     for (int u = 0; u < LU; ++u)
       reinterpret_cast<u32x4*>(S0 + STAGE + (wave * LU + u) * 1024)[lane] = u32x4{};
     __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));   // in LDS before barrier 0
-    dma_k(S0, p0);
-    dma_k(S1, p1);
-    dma_v(S1 + STAGE, p0);
-    dma_k(S2, vp);
-    dma_v(S2 + STAGE, p1);
+#pragma unroll
+    for (int u = 0; u < LU; ++u) dma_k(S0, p0, u);
+#pragma unroll
+    for (int u = 0; u < LU; ++u) { dma_k(S1, p1, u); dma_v(S1 + STAGE, p0, u); }
+#pragma unroll
+    for (int u = 0; u < LU; ++u) { dma_k(S2, kp, u); dma_v(S2 + STAGE, p1, u); }
   }
   // the stages of a wave without rows (its share of the loads, and the barriers),
   // of the first group, or of the second
   auto run = [&](auto works, auto late, auto Half) {
     constexpr bool WORKS = decltype(works)::value, LATE = decltype(late)::value;
-    // slot j: a stage, or behind the last one nothing but the barrier and its DMA
-    // (which then brings the last stage again, to where it is or nobody reads)
-    auto slot = [&](auto J, int j) {
-      if constexpr (!LATE) meet(J, j);
-      if constexpr (WORKS)
-        if (j < stages) {
-          __builtin_amdgcn_s_setprio(1);
-          products(yes, Half, J);
-          __builtin_amdgcn_s_setprio(0);
-        }
-      if constexpr (LATE) meet(std::integral_constant<int, (decltype(J)::value + 1) & 3>{}, j + 1);
-      if constexpr (WORKS)
-        if (j < stages) softmax(Half);
-    };
-    if constexpr (LATE) meet(i0, 0);
-    for (int j = 0; j < stages; j += 4) {
-      slot(i0, j);
-      slot(i1, j + 1);
-      slot(i2, j + 2);
-      slot(i3, j + 3);
-    }
-    if constexpr (!LATE) {   // as many barriers as the other group's
-      wait_vmcnt<0>();
-      __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_barrier();
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    if constexpr (WORKS) {   // the last stage's values
-      switch (stages & 3) {
-        case 0: products(no, Half, i0); break;
-        case 1: products(no, Half, i1); break;
-        case 2: products(no, Half, i2); break;
-        default: products(no, Half, i3);
+    auto stage = [&](auto J, int j) {
+      if constexpr (!LATE) meet(j);
+      if constexpr (WORKS) {
+        __builtin_amdgcn_s_setprio(1);
+        products(yes, Half, J);
+        __builtin_amdgcn_s_setprio(0);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 2 * LU; ++q) start(J, q);
       }
+      if constexpr (LATE) meet(j + 1);
+      if constexpr (WORKS) softmax(Half);
+    };
+    if constexpr (LATE) meet(0);
+    for (int j = 0; j < stages; j += 4) {   // whole fours
+      stage(i0, j);
+      stage(i1, j + 1);
+      stage(i2, j + 2);
+      stage(i3, j + 3);
     }
+    if constexpr (!LATE) meet(stages);      // as many barriers as the other group's
+    if constexpr (WORKS) products(no, Half, i0);
   };
   if (!active) run(no, no, i2);
   else if (wave < NW / 2) { if (split) run(yes, no, i0); else run(yes, no, i2); }
