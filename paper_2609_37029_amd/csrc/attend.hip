@@ -754,7 +754,8 @@ template <int C> __device__ inline int turn(int r) {
 #define LDR_GP(p) ((__attribute__((address_space(1))) void*)(p))
 #define LDR_LP(p) ((__attribute__((address_space(3))) void*)(p))
 
-template <int D>
+// SMALL: pages of 32 rows, half a stage.
+template <int D, bool SMALL>
 __global__ void __launch_bounds__(kWideThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 attend_wide_kernel(AttendArgs a) {
   using M = Mma<uint16_t>;
@@ -796,7 +797,6 @@ attend_wide_kernel(AttendArgs a) {
   // DMA. A half stage starts a page of 32, a stage lies at a multiple of 64 of a
   // larger one: the lanes' offsets in it stay.
   const int shift = 31 - __builtin_clz(a.s.page);
-  const bool small = shift == 5;
   uint32_t koff[LU], voff[LU];
   bool second[LU];     // the lane's V is of keys 32 ..
 #pragma unroll
@@ -804,8 +804,8 @@ attend_wide_kernel(AttendArgs a) {
     const int n = wave * LU + u;
     const int kr = n * (64 / KC) + lane / KC, vr = n * (64 / VC) + lane / VC;
     const int kc = (lane % KC) ^ turn<KC>(kr), vc = (lane % VC) ^ turn<VC>(vr);
-    koff[u] = ((small ? kr & 31 : kr) * D + kc * 8) * 2;
-    voff[u] = (vr * a.s.page + (small ? (vc & 3) * 8 : vc * 8)) * 2;
+    koff[u] = ((SMALL ? kr & 31 : kr) * D + kc * 8) * 2;
+    voff[u] = (vr * a.s.page + (SMALL ? (vc & 3) * 8 : vc * 8)) * 2;
     second[u] = vc >= 4;
   }
   // where a stage's keys are: elements from the pool's start to its page (and, of
@@ -814,26 +814,28 @@ attend_wide_kernel(AttendArgs a) {
   struct Ids { int a, b; };
   auto ids_of = [&](int j) {     // on their way until they are looked at
     const int k = it.k0 + j * kStage;
-    return Ids{scalar_word(table, k >> shift), small ? scalar_word(table, (k + 32) >> shift) : 0};
+    return Ids{scalar_word(table, k >> shift), SMALL ? scalar_word(table, (k + 32) >> shift) : 0};
   };
   auto place = [&](Ids ids, int j) {
     Place p;
     p.a = (size_t)clamp_page(a.s, ids.a) * page_el;
-    p.b = small ? (size_t)clamp_page(a.s, ids.b) * page_el : p.a;
-    p.in = small ? 0 : (it.k0 + j * kStage) & (a.s.page - 1);
+    p.b = SMALL ? (size_t)clamp_page(a.s, ids.b) * page_el : p.a;
+    p.in = SMALL ? 0 : (it.k0 + j * kStage) & (a.s.page - 1);
     return p;
+  };
+  auto dma = [&](uint8_t* to, const uint16_t* base, uint32_t off) {
+    const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), 0, 0x7fffffff,
+                                                        0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, LDR_LP(to), 16, off, 0, 0, 0);
   };
   auto dma_k = [&](uint8_t* to, const Place& p, int u) {
     const int n = wave * LU + u;
-    const uint8_t* from =
-        reinterpret_cast<const uint8_t*>(kpool + (n * (64 / KC) < 32 ? p.a : p.b) + p.in * D);
-    __builtin_amdgcn_global_load_lds(LDR_GP(from + koff[u]), LDR_LP(to + n * 1024), 16, 0, 0);
+    dma(to + n * 1024, kpool + (n * (64 / KC) < 32 ? p.a : p.b) + p.in * D, koff[u]);
   };
   auto dma_v = [&](uint8_t* to, const Place& p, int u) {
-    const uint8_t* from = reinterpret_cast<const uint8_t*>(vpool + p.a + p.in);
-    const size_t apart = small && second[u] ? (p.b - p.a) * 2 : 0;
-    __builtin_amdgcn_global_load_lds(LDR_GP(from + apart + voff[u]),
-                                     LDR_LP(to + (wave * LU + u) * 1024), 16, 0, 0);
+    to += (wave * LU + u) * 1024;
+    if (SMALL && second[u]) dma(to, vpool + p.b + p.in, voff[u]);
+    else dma(to, vpool + p.a + p.in, voff[u]);
   };
   auto buffer = [&](auto i) -> uint8_t* {
     constexpr int I = decltype(i)::value & 3;
@@ -1050,7 +1052,10 @@ template <typename T, int D>
 hipError_t launch(const AttendArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)a.w.max_items * a.s.hkv);
   if constexpr (sizeof(T) == 2)
-    hipLaunchKernelGGL(attend_wide_kernel<D>, grid, dim3(kWideThreads), 0, st, a);
+    if (a.s.page < kStage)
+      hipLaunchKernelGGL((attend_wide_kernel<D, true>), grid, dim3(kWideThreads), 0, st, a);
+    else
+      hipLaunchKernelGGL((attend_wide_kernel<D, false>), grid, dim3(kWideThreads), 0, st, a);
   else
     hipLaunchKernelGGL((attend_rows_kernel<T, D, false>), grid, dim3(kThreads), 0, st, a);
   hipError_t e = hipGetLastError();
