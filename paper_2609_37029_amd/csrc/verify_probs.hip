@@ -1,25 +1,27 @@
 // Speculative verification from given probabilities and uniforms (Eq. 1-2).
 //
-// Two launches. The first has one workgroup per (part of the vocabulary,
-// sequence): each takes the in-order acceptance test itself (block gathered
-// pairs of probabilities), then sums its part of the target row where the round
-// stops, and of the residual, in fp64. The second, one workgroup per sequence,
-// finds the part in which the cumulative sum passes u C and the token inside it.
+// Two launches. The first has one workgroup per (run of parts of 1024 tokens, a
+// wave a part; sequence): each takes the in-order acceptance test itself (block gathered pairs
+// of probabilities), then sums its parts of the target row where the round stops,
+// and of the residual, in fp64. The second, one workgroup per sequence, finds the
+// part in which the cumulative sum passes u C and the token inside it.
 //
 // fp64: differences of fp32 numbers and sums of 150 thousand of them lose nothing
 // that a draw could see, so the token does not depend on how the sum is cut up.
 // The test u q < p compares a 48-bit product exactly.
 //
 // Bound by reading one target and one draft row a sequence, once, and at small
-// batches by the latency of the chain: gathers, rows, sums, second launch.
+// batches by the latency of the chain: tokens, gathers, rows, sums, second launch,
+// part.
 #include "ldr_internal.h"
 
 namespace ldr {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPart = 4096;            // tokens of a part
-constexpr int kEach = kPart / kThreads;
+constexpr int kPart = 1024;            // tokens of a part
+constexpr int kEach = kPart / kThreads;    // tokens of a part a thread draws from
+constexpr int kLane = kPart / 64;          // and a lane sums
 
 struct Part { double res, tgt; };      // sums of [p - q]_+ and p over a part
 
@@ -30,6 +32,7 @@ struct ProbsArgs {
   const int32_t* n;      // [batch] or null
   const float* u;        // [batch][B + 1]
   int batch, B, V, parts;
+  int run;               // parts of a wave of the first launch
   Part* part;            // [batch][parts]
   int32_t* accepted; int32_t* token; int32_t* n_new;
 };
@@ -77,8 +80,9 @@ __device__ inline Row row_of(const ProbsArgs& a, int b, const Stop& s) {
   }
   return w;
 }
-__device__ inline double residual(const Row& w, double p, int v) {
-  return positive(p - (w.q ? (double)w.q[v] : v == w.y ? 1.0 : 0.0));
+// w_v of the residual from p and q at v, and of p alone.
+__device__ inline double residual(const Row& w, float p, float q, int v) {
+  return positive((double)p - (w.q ? (double)q : v == w.y ? 1.0 : 0.0));
 }
 
 __device__ inline double wave_sum(double v) {
@@ -86,102 +90,147 @@ __device__ inline double wave_sum(double v) {
   for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
   return v;
 }
+// The sum over the threads up to this one, and over all.
+__device__ inline double block_scan(double v, double* sums, double* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  double inc = v;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const double o = __shfl_up(inc, off);
+    if (lane >= off) inc += o;
+  }
+  __syncthreads();
+  if (lane == 63) sums[wave] = inc;
+  __syncthreads();
+  double before = 0.0, all = 0.0;
+#pragma unroll
+  for (int k = 0; k < kThreads / 64; ++k) {
+    before += k < wave ? sums[k] : 0.0;
+    all += sums[k];
+  }
+  *total = all;
+  return before + inc;
+}
 
+// VEC: rows start on 16 bytes and V is a multiple of 4.
+template <bool VEC>
 __global__ void __launch_bounds__(kThreads) probs_sum_kernel(ProbsArgs a) {
-  const int b = blockIdx.y, v0 = blockIdx.x * kPart;
+  const int b = blockIdx.y, lane = threadIdx.x & 63;
   const Stop s = find_stop(a, b);
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     a.accepted[b] = s.r;
     a.n_new[b] = s.r + 1;
   }
   const Row w = row_of(a, b, s);
-  double res = 0.0, tgt = 0.0;
+  const int first = (blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)) * a.run;
+  const int last = min(first + a.run, a.parts);
+  constexpr int W = VEC ? 4 : 1;
+  for (int c = first; c < last; ++c) {
+    const int v0 = c * kPart + lane * W;
+    float p[kLane], q[kLane];
 #pragma unroll
-  for (int k = 0; k < kEach; ++k) {
-    const int v = v0 + k * kThreads + threadIdx.x;
-    if (v < a.V) {
-      const double p = w.p[v];
-      tgt += positive(p);
-      if (s.rejected) res += residual(w, p, v);
+    for (int k = 0; k < kLane; k += W) {
+      const int v = v0 + k * 64;
+      const bool in = v < a.V;
+      if constexpr (VEC) {
+        const float4 z{0.f, 0.f, 0.f, 0.f};
+        *reinterpret_cast<float4*>(p + k) = in ? *reinterpret_cast<const float4*>(w.p + v) : z;
+        *reinterpret_cast<float4*>(q + k) = in && w.q ? *reinterpret_cast<const float4*>(w.q + v) : z;
+      } else {
+        p[k] = in ? w.p[v] : 0.f;
+        q[k] = in && w.q ? w.q[v] : 0.f;
+      }
     }
-  }
-  res = wave_sum(res);
-  tgt = wave_sum(tgt);
-  __shared__ Part red[kThreads / 64];
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = Part{res, tgt};
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    Part t{0.0, 0.0};
-    for (int k = 0; k < kThreads / 64; ++k) { t.res += red[k].res; t.tgt += red[k].tgt; }
-    a.part[(size_t)b * a.parts + blockIdx.x] = t;
+    double res = 0.0, tgt = 0.0;
+#pragma unroll
+    for (int k = 0; k < kLane; ++k) {
+      tgt += positive(p[k]);
+      if (s.rejected) res += residual(w, p[k], q[k], v0 + k / W * W * 64 + k % W);
+    }
+    res = wave_sum(res);
+    tgt = wave_sum(tgt);
+    if (lane == 0) a.part[(size_t)b * a.parts + c] = Part{res, tgt};
   }
 }
 
+template <bool VEC>
 __global__ void __launch_bounds__(kThreads) probs_draw_kernel(ProbsArgs a) {
-  __shared__ double sums[kThreads];
-  __shared__ double before;
-  __shared__ int part, found, last;
+  __shared__ double sums[kThreads / 64];
+  __shared__ double before[2];        // of the part that holds the draw, and of the last one
+  __shared__ int part, last_part, found, last;
   const int b = blockIdx.x, tid = threadIdx.x;
   const int r = a.accepted[b];
   const int n = a.n ? min(max(a.n[b], 0), a.B) : a.B;
+  const double u = a.u[(size_t)b * (a.B + 1) + a.B];
   const Stop s{r, r < n};
   const Row w = row_of(a, b, s);
   const Part* pt = a.part + (size_t)b * a.parts;
-  if (tid == 0) {
-    bool use = false;
-    for (int c = 0; c < a.parts; ++c) use = use || pt[c].res > 0.0;
-    double total = 0.0;
-    for (int c = 0; c < a.parts; ++c) total += use ? pt[c].res : pt[c].tgt;
-    const double t = (double)a.u[(size_t)b * (a.B + 1) + a.B] * total;
-    double sum = 0.0;
-    int at = -1, final = -1;
-    double at_before = 0.0, final_before = 0.0;
-    for (int c = 0; c < a.parts; ++c) {
-      const double x = use ? pt[c].res : pt[c].tgt;
-      if (x > 0.0) {
-        if (at < 0 && sum + x > t) { at = c; at_before = sum; }
-        final = c;
-        final_before = sum;
-      }
-      sum += x;
+  if (tid == 0) { part = a.parts; last_part = -1; found = a.V; last = -1; }
+  // a run of consecutive parts a thread
+  const int each = (a.parts + kThreads - 1) / kThreads;
+  const int c0 = min(tid * each, a.parts), c1 = min(c0 + each, a.parts);
+  double res = 0.0, tgt = 0.0;
+  for (int c = c0; c < c1; ++c) { res += pt[c].res; tgt += pt[c].tgt; }
+  const bool use = __syncthreads_or(res > 0.0);
+  double total = 0.0;
+  double cum = block_scan(use ? res : tgt, sums, &total) - (use ? res : tgt);
+  const double t = u * total;
+  int at = -1, final = -1;
+  double at_before = 0.0, final_before = 0.0;
+  for (int c = c0; c < c1; ++c) {
+    const double x = use ? pt[c].res : pt[c].tgt;
+    if (x > 0.0) {
+      if (at < 0 && cum + x > t) { at = c; at_before = cum; }
+      final = c;
+      final_before = cum;
     }
-    part = at >= 0 ? at : final;
-    before = at >= 0 ? at_before : final_before;
-    sums[0] = t;
-    found = a.V;
-    last = use ? 1 : 0;
+    cum += x;
   }
+  if (at >= 0) atomicMin(&part, at);
+  if (final >= 0) atomicMax(&last_part, final);
   __syncthreads();
-  const double t = sums[0];
-  const bool use = last;
-  const int c = part;
+  if (at >= 0 && part == at) before[0] = at_before;
+  if (final >= 0 && last_part == final) before[1] = final_before;
   __syncthreads();
+  const bool hit_part = part < a.parts;
+  const int c = hit_part ? part : last_part;
   if (c < 0) {   // no entry above 0
     if (tid == 0) a.token[b] = 0;
     return;
   }
   // kEach consecutive tokens a thread
   const int v0 = c * kPart + tid * kEach;
+  static_assert(kEach == 4, "16 bytes");
+  float p[kEach] = {}, q[kEach] = {};
+  if constexpr (VEC) {
+    if (v0 < a.V) {
+      *reinterpret_cast<float4*>(p) = *reinterpret_cast<const float4*>(w.p + v0);
+      if (w.q) *reinterpret_cast<float4*>(q) = *reinterpret_cast<const float4*>(w.q + v0);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      if (v0 + k < a.V) {
+        p[k] = w.p[v0 + k];
+        if (w.q) q[k] = w.q[v0 + k];
+      }
+    }
+  }
   double x[kEach], sum = 0.0;
   int end = -1;
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
-    const int v = v0 + k;
-    const double p = v < a.V ? (double)w.p[v] : 0.0;
-    x[k] = v < a.V ? (use ? residual(w, p, v) : positive(p)) : 0.0;
-    if (x[k] > 0.0) end = v;
+    x[k] = use ? residual(w, p[k], q[k], v0 + k) : positive(p[k]);   // 0 behind the row
+    if (x[k] > 0.0) end = v0 + k;
     sum += x[k];
   }
-  sums[tid] = sum;
-  if (tid == 0) last = -1;
-  __syncthreads();
-  double cum = before;
-  for (int k = 0; k < tid; ++k) cum += sums[k];
+  double all = 0.0;
+  double run = before[hit_part ? 0 : 1] + block_scan(sum, sums, &all) - sum;
   int hit = a.V;
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
-    cum += x[k];
-    if (hit == a.V && x[k] > 0.0 && cum > t) hit = v0 + k;
+    run += x[k];
+    if (hit == a.V && x[k] > 0.0 && run > t) hit = v0 + k;
   }
   if (hit < a.V) atomicMin(&found, hit);
   if (end >= 0) atomicMax(&last, end);
@@ -199,12 +248,22 @@ hipError_t launch_verify_probs(const float* P, const float* Q, const int32_t* y,
                                const int32_t* n_draft, const float* u, int batch, int B, int V,
                                int32_t* accepted, int32_t* token, int32_t* n_new, void* ws,
                                hipStream_t st) {
-  ProbsArgs a{P, Q, y, n_draft, u, batch, B, V, (V + kPart - 1) / kPart,
-              static_cast<Part*>(ws), accepted, token, n_new};
-  hipLaunchKernelGGL(probs_sum_kernel, dim3(a.parts, batch), dim3(kThreads), 0, st, a);
+  const int parts = (V + kPart - 1) / kPart;
+  // each workgroup tests the candidates first: few workgroups a sequence, as long as
+  // all of them fill the GPU
+  const int run = max(1, min(8, (int)((long)parts * batch / 3072)));
+  ProbsArgs a{P, Q, y, n_draft, u, batch, B, V, parts, run, static_cast<Part*>(ws), accepted, token,
+              n_new};
+  const bool vec = V % 4 == 0 && reinterpret_cast<uintptr_t>(P) % 16 == 0 &&
+                   reinterpret_cast<uintptr_t>(Q) % 16 == 0;
+  const int wg = run * (kThreads / 64);    // parts of a workgroup
+  const dim3 grid((parts + wg - 1) / wg, batch);
+  if (vec) hipLaunchKernelGGL(probs_sum_kernel<true>, grid, dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL(probs_sum_kernel<false>, grid, dim3(kThreads), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(probs_draw_kernel, dim3(batch), dim3(kThreads), 0, st, a);
+  if (vec) hipLaunchKernelGGL(probs_draw_kernel<true>, dim3(batch), dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL(probs_draw_kernel<false>, dim3(batch), dim3(kThreads), 0, st, a);
   return hipGetLastError();
 }
 
