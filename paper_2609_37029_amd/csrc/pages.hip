@@ -163,60 +163,78 @@ __device__ inline void copy_piece(const PagesShape& s, const PagesPtrs& p, int p
   }
 }
 
-// The copies that a reserve asked for: at most one page a sequence.
+// The copies that a reserve asked for, at most one page a sequence: of its rows
+// before the open ones, one workgroup per (head, layer's K or V, sequence). Whole
+// pages would be 7 times the bytes where 9 rows of 64 are used (64 forks of the
+// Qwen3-8B cache, 26 us).
 __global__ void __launch_bounds__(kThreads) pages_part_kernel(PagesShape s, PagesPtrs p) {
-  const int b = blockIdx.z;
+  const int b = blockIdx.z, plane = blockIdx.y;
   const int from = p.state[s.pairs + 2 * b], to = p.state[s.pairs + 2 * b + 1];
   if (from < 0 || from >= s.n_pages || to < 0 || to >= s.n_pages) return;
-  copy_piece(s, p, blockIdx.y, blockIdx.x, from, to);
+  const int part = max(p.state[s.rows + b] - p.state[s.open + b], 0) % s.page;
+  const size_t head = (size_t)s.page * s.d * s.el;
+  const uint8_t* base = p.pool + (size_t)plane * s.n_pages * s.page_bytes + blockIdx.x * head;
+  const uint4* in = reinterpret_cast<const uint4*>(base + (size_t)from * s.page_bytes);
+  uint4* out = reinterpret_cast<uint4*>(const_cast<uint8_t*>(base) + (size_t)to * s.page_bytes);
+  // K: `part` rows; V: as many columns, rounded up to 16 bytes, of head_dim rows
+  const int e = 16 / (int)s.el, width = (part + e - 1) / e, pitch = s.page / e;
+  const int n = plane & 1 ? s.d * width : part * s.d / e;
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const int at = plane & 1 ? i / width * pitch + i % width : i;
+    out[at] = in[at];
+  }
 }
 
-// Open rows into their pages: one workgroup per (tile of 32 rows inside a page,
-// layer and head, sequence). K rows are copied; V is transposed through LDS, so
-// that a thread stores a run of up to 8 rows of one dimension.
+// Open rows into their pages: one workgroup per (32 positions, layer and head,
+// sequence), on two pages at most. K rows are copied; V is transposed through LDS
+// and stored by runs of 16 bytes of one dimension. Tiles begin at multiples of such
+// a run, so that no two workgroups write to one; the first and the last run keep
+// their other rows, which nobody else writes (the page is the sequence's own).
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 pages_write_kernel(PagesShape s, PagesPtrs p, int layer0, int n_layers, const T* K, const T* V,
                    int max_new) {
-  constexpr int RT = 32, E = 16 / (int)sizeof(T), LD = 128 + E;
+  constexpr int RT = 32, E = 16 / (int)sizeof(T), LD = 128 + E, RUNS = RT / E;
   __shared__ alignas(16) T tile[RT * LD];
   const int b = blockIdx.z, h = blockIdx.y % s.hkv, l = blockIdx.y / s.hkv;
   const int rows = clamp_rows(s, p.state[s.rows + b]);
   const int open = min(max(p.state[s.open + b], 0), rows);
-  const int n = min(open, max_new);
-  const int pos0 = rows - open;
-  const int t0 = (pos0 / RT + (int)blockIdx.x) * RT;    // first position of the tile
-  const int lo = max(t0, pos0), hi = min(t0 + RT, pos0 + n);
-  if (lo >= hi) return;
-  const int id = clamp_page(s, p.state[s.table + (size_t)b * s.max_pages + t0 / s.page]);
+  const int start = rows - open, end = start + min(open, max_new);
+  const int first = start / E * E + (int)blockIdx.x * RT;
+  if (first >= end) return;
+  const int lo = max(first, start), hi = min(first + RT, end), cnt = hi - lo;
+  const int32_t* table = p.state + s.table + (size_t)b * s.max_pages;
+  const int j0 = lo / s.page;
+  const int id0 = clamp_page(s, table[j0]), id1 = clamp_page(s, table[(hi - 1) / s.page]);
   const size_t plane = (size_t)2 * (layer0 + l) * s.n_pages;
   const size_t head = (size_t)h * s.page * s.d;
-  T* kp = reinterpret_cast<T*>(p.pool + (plane + id) * s.page_bytes) + head;
-  T* vp = reinterpret_cast<T*>(p.pool + (plane + s.n_pages + id) * s.page_bytes) + head;
+  uint8_t* kpool = p.pool + plane * s.page_bytes;
+  uint8_t* vpool = kpool + (size_t)s.n_pages * s.page_bytes;
+  auto page = [&](uint8_t* pool, int pos) {     // of a position of the tile
+    return reinterpret_cast<T*>(pool + (size_t)(pos / s.page == j0 ? id0 : id1) * s.page_bytes) + head;
+  };
   const size_t row = (size_t)n_layers * s.hkv * s.d;
-  const size_t in0 = ((size_t)b * max_new + (lo - pos0)) * row + ((size_t)l * s.hkv + h) * s.d;
-  const int c = s.d / E, cnt = hi - lo;                 // 16-byte pieces of a row
+  const size_t in0 = ((size_t)b * max_new + (lo - start)) * row + ((size_t)l * s.hkv + h) * s.d;
+  const int c = s.d / E;                        // 16-byte pieces of a row
   for (int i = threadIdx.x; i < cnt * c; i += kThreads) {
     const int r = i / c, e = (i - r * c) * E;
-    *reinterpret_cast<uint4*>(kp + (size_t)(lo + r) % s.page * s.d + e) =
+    *reinterpret_cast<uint4*>(page(kpool, lo + r) + (size_t)(lo + r) % s.page * s.d + e) =
         *reinterpret_cast<const uint4*>(K + in0 + r * row + e);
-    *reinterpret_cast<uint4*>(tile + (lo - t0 + r) * LD + e) =
+    *reinterpret_cast<uint4*>(tile + r * LD + e) =
         *reinterpret_cast<const uint4*>(V + in0 + r * row + e);
   }
   __syncthreads();
-  const int off = t0 % s.page;                          // multiple of 32
-  for (int i = threadIdx.x; i < s.d * (RT / E); i += kThreads) {
-    const int dim = i / (RT / E), r0 = (i - dim * (RT / E)) * E;   // E rows of one dimension
-    T* out = vp + (size_t)dim * s.page + off + r0;
-    if (t0 + r0 >= lo && t0 + r0 + E <= hi) {
-      alignas(16) T x[E];
+  for (int i = threadIdx.x; i < s.d * RUNS; i += kThreads) {
+    const int dim = i / RUNS, pos = first + (i - dim * RUNS) * E;
+    if (pos >= hi) continue;
+    uint4* out = reinterpret_cast<uint4*>(page(vpool, max(pos, lo)) + (size_t)dim * s.page +
+                                          pos % s.page);
+    alignas(16) T x[E];
+    if (pos < lo || pos + E > hi) *reinterpret_cast<uint4*>(x) = *out;
 #pragma unroll
-      for (int k = 0; k < E; ++k) x[k] = tile[(r0 + k) * LD + dim];
-      *reinterpret_cast<uint4*>(out) = *reinterpret_cast<const uint4*>(x);
-    } else {
-      for (int k = 0; k < E; ++k)
-        if (t0 + r0 + k >= lo && t0 + r0 + k < hi) out[k] = tile[(r0 + k) * LD + dim];
-    }
+    for (int k = 0; k < E; ++k)
+      if (pos + k >= lo && pos + k < hi) x[k] = tile[(pos + k - lo) * LD + dim];
+    *out = *reinterpret_cast<const uint4*>(x);
   }
 }
 
@@ -368,15 +386,15 @@ hipError_t launch_pages_reserve(const PagesShape& s, const PagesPtrs& p, const i
   hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(kBook), 0, st, s, p, n_new, max_new);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(pages_part_kernel, dim3(pieces_of(s), 2 * s.layers, s.batch), dim3(kThreads),
-                     0, st, s, p);
+  hipLaunchKernelGGL(pages_part_kernel, dim3(s.hkv, 2 * s.layers, s.batch), dim3(kThreads), 0, st, s,
+                     p);
   return hipGetLastError();
 }
 
 hipError_t launch_pages_write(const PagesShape& s, const PagesPtrs& p, int layer, int n_layers,
                               const void* K, const void* V, int max_new, hipStream_t st) {
-  // max_new rows lie in at most this many tiles of 32 positions
-  const dim3 grid((max_new + 30) / 32 + 1, n_layers * s.hkv, s.batch);
+  // tiles begin at a multiple of 16 bytes, up to a run less one before the rows
+  const dim3 grid((max_new + 16 / (int)s.el + 30) / 32, n_layers * s.hkv, s.batch);
   if (s.dtype == LDR_BF16)
     hipLaunchKernelGGL(pages_write_kernel<uint16_t>, grid, dim3(kThreads), 0, st, s, p, layer,
                        n_layers, static_cast<const uint16_t*>(K),
