@@ -451,6 +451,15 @@ __device__ inline float other_half(float x) {
 __device__ inline float half_max(float x) { return fmaxf(x, other_half(x)); }
 __device__ inline float half_sum(float x) { return x + other_half(x); }
 
+// The value of the column 16, 8, 4, 2 or 1 to the side, of the same half. By turns
+// for 8 and 4: of columns that agree at twice the distance, that is the same.
+template <int OFF> __device__ inline float aside(float x) {
+  const int v = __float_as_int(x);
+  if constexpr (OFF == 16) return __int_as_float(__builtin_amdgcn_ds_swizzle(v, 0x401f));
+  else return __int_as_float(__builtin_amdgcn_update_dpp(
+      0, v, OFF == 8 ? 0x128 : OFF == 4 ? 0x124 : OFF == 2 ? 0x4e : 0xb1, 0xf, 0xf, true));
+}
+
 // V where a mask crosses a step: keys from k1 on hold anything and count as 0. A
 // value that is not finite but masked for some rows only would reach them as
 // 0 x inf: it is taken out here (true: there was one), to be added to the rows
@@ -520,7 +529,8 @@ attend_rows_kernel(AttendArgs a) {
     if (!plan_ok(a, items) || unit >= items || it.k1 <= it.k0) return;
   }
   const int32_t* map = reinterpret_cast<const int32_t*>(a.ws + a.w.map);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int32_t* table = a.p.state + a.s.table + (size_t)it.seq * a.s.max_pages;
   const size_t plane = (size_t)2 * a.layer * a.s.n_pages * a.s.page_bytes;
@@ -545,35 +555,39 @@ attend_rows_kernel(AttendArgs a) {
   bool bad = false;   // V held a value that is not finite where a mask is
 
   const int steps = (max(it.k1 - it.k0, 0) + kStep - 1) / kStep;
-  int ids = 0;    // the pages of this wave's next 64 steps, one a lane
+  const int shift = 31 - __builtin_clz(a.s.page);
+  auto id_of = [&](int t) {   // the page of the wave's step t, on its way until it is looked at
+    return scalar_word(table, (it.k0 + min(t * W + wave, max(steps - 1, 0)) * kStep) >> shift);
+  };
   u32x4 kf[NF];
   const T* vbase = nullptr;
+  int id = wave < steps ? id_of(0) : 0;
   auto fetch = [&](int t) {   // K of the wave's step t; where its V is
-    const int st = t * W + wave;
-    if ((t & 63) == 0) {
-      const int sl = min((t + lane) * W + wave, steps - 1);
-      ids = clamp_page(a.s, table[(it.k0 + sl * kStep) / a.s.page]);
-    }
-    const int k = it.k0 + st * kStep;
-    const size_t off = (size_t)__builtin_amdgcn_readlane(ids, t & 63) * a.s.page_bytes;
-    const int in = k & (a.s.page - 1);
+    const size_t off = (size_t)clamp_page(a.s, id) * a.s.page_bytes;
+    const int in = (it.k0 + (t * W + wave) * kStep) & (a.s.page - 1);
     const T* kp = reinterpret_cast<const T*>(kpool + off) + hoff + (size_t)(in + krow) * D;
 #pragma unroll
     for (int i = 0; i < NF; ++i) kf[i] = *reinterpret_cast<const u32x4*>(kp + (2 * i + half) * E);
     vbase = reinterpret_cast<const T*>(vpool + off) + hoff + in + half * E;
+    id = id_of(t + 1);
   };
   if (wave < steps) fetch(0);
   if constexpr (FINISH) {
-    // parts: the group's chunks, then the tile's own
+    // parts: the group's chunks, then the tile's own. Of few rows there are columns
+    // to spare: R a part, and 32 / R parts at a time (4 rows of 32 parts, as 64
+    // sequences with one token each have, took 8 loads behind one another, 11 us).
     const int t = it.r0 / tile_of(a.s).rows * tile_of(a.s).rows;
     const int own = f.own_chunks
                         ? (tile_keys(f.rows, f.open, f.share, t, a.rep, tile_of(a.s).unit) + f.step - 1) / f.step : 0;
-    const int gr = f.grp_off + r;
-    for (int c = wave; c < f.grp_chunks + own; c += W) {
+    const int parts = f.grp_chunks + own;
+    int R = 32;
+    while (R > 1 && 2 * it.nr <= R && W * 32 < parts * R) R >>= 1;
+    const int rp = it.r0 + min(col & (R - 1), it.nr - 1), gr = f.grp_off + rp;
+    for (int c = wave + W * (col / R); c < parts; c += W * (32 / R)) {
       const bool g = c < f.grp_chunks;
       const long block = g ? f.grp_part + (long)c * f.grp_blocks + gr / kBlock
                            : f.own_part + (long)(c - f.grp_chunks) * f.own_blocks + it.r0 / kBlock;
-      const int at = g ? gr % kBlock : r % kBlock;
+      const int at = g ? gr % kBlock : rp % kBlock;
       const float2 ml = part_ml(a, head, block)[at];
       const float4* po = reinterpret_cast<const float4*>(part_o<D>(a, head, block)) + half * 32 + at;
       float4 v[D / 8];
@@ -592,6 +606,31 @@ attend_rows_kernel(AttendArgs a) {
         o[dt][q + 2] = o[dt][q + 2] * wo + v[i].z * wp;
         o[dt][q + 3] = o[dt][q + 3] * wo + v[i].w * wp;
       }
+    }
+    if (R < 32) {            // the columns of a row, to their common maximum and added up
+      float mn = fmaxf(m, aside<16>(m));
+      if (R < 16) mn = fmaxf(mn, aside<8>(mn));
+      if (R < 8) mn = fmaxf(mn, aside<4>(mn));
+      if (R < 4) mn = fmaxf(mn, aside<2>(mn));
+      if (R < 2) mn = fmaxf(mn, aside<1>(mn));
+      const float w = __builtin_amdgcn_exp2f((m - (mn == -INFINITY ? 0.f : mn)) * c2);
+      m = mn;
+      l *= w;
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) o[dt] *= w;
+      auto add = [&](auto off) {
+        constexpr int OFF = decltype(off)::value;
+        l += aside<OFF>(l);
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[dt][i] += aside<OFF>(o[dt][i]);
+      };
+      add(std::integral_constant<int, 16>{});
+      if (R < 16) add(std::integral_constant<int, 8>{});
+      if (R < 8) add(std::integral_constant<int, 4>{});
+      if (R < 4) add(std::integral_constant<int, 2>{});
+      if (R < 2) add(std::integral_constant<int, 1>{});
     }
     l = half ? 0.f : l;      // of both halves; the steps' sums are of one each
   }
@@ -673,46 +712,66 @@ attend_rows_kernel(AttendArgs a) {
                  o[dt][4 * g + 3] * own};
   __syncthreads();
   // thread i: values e .. e + 3 of a row; rows fastest for a part's order
-  for (int i = threadIdx.x; i < 32 * (D / 4); i += kThreads) {
-    const int row = FINISH ? i / (D / 4) : i % 32, e = FINISH ? i % (D / 4) * 4 : i / 32 * 4;
-    if (FINISH && row >= it.nr) break;
-    float mm = sm[0][row];
+  constexpr int NI = 32 * (D / 4) / kThreads;
+  auto row_of = [](int i) { return FINISH ? i / (D / 4) : i % 32; };
+  auto el_of = [](int i) { return FINISH ? i % (D / 4) * 4 : i / 32 * 4; };
+  float acc[NI][4], ll[NI], mm[NI];
 #pragma unroll
-    for (int k = 1; k < W; ++k) mm = fmaxf(mm, sm[k][row]);
-    const float mz = mm == -INFINITY ? 0.f : mm;
-    float ll = 0.f, acc[4] = {};
+  for (int u = 0; u < NI; ++u) {
+    const int i = u * kThreads + threadIdx.x, row = row_of(i), e = el_of(i);
+    mm[u] = sm[0][row];
+#pragma unroll
+    for (int k = 1; k < W; ++k) mm[u] = fmaxf(mm[u], sm[k][row]);
+    const float mz = mm[u] == -INFINITY ? 0.f : mm[u];
+    ll[u] = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[u][k] = 0.f;
 #pragma unroll
     for (int k = 0; k < W; ++k) {
-      ll += sl[k][row] * __builtin_amdgcn_exp2f((sm[k][row] - mz) * c2);
+      ll[u] += sl[k][row] * __builtin_amdgcn_exp2f((sm[k][row] - mz) * c2);
       const float4 v = *reinterpret_cast<const float4*>(&so[k][row * LD + e]);
-      acc[0] += v.x; acc[1] += v.y; acc[2] += v.z; acc[3] += v.w;
+      acc[u][0] += v.x; acc[u][1] += v.y; acc[u][2] += v.z; acc[u][3] += v.w;
     }
     if constexpr (FINISH) {
-      const int rr = it.r0 + row, q = rr / a.rep;
-      const size_t at = ((size_t)it.seq * a.max_new + q) * a.hq + head * a.rep + (rr - q * a.rep);
-      const float inv = ll == 0.f ? 0.f : 1.f / ll;
+      const float inv = ll[u] == 0.f ? 0.f : 1.f / ll[u];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) acc[k] *= inv;
-      if (odd[0] | odd[1] | odd[2] | odd[3]) {   // what clean_values took out
-        const int s0 = max(0, cbase + it.r0 / a.rep + 1 - it.k0) / kStep;
-        for (int k = it.k0 + s0 * kStep; k <= cbase + q; ++k) {
+      for (int k = 0; k < 4; ++k) acc[u][k] *= inv;
+    }
+  }
+  if constexpr (FINISH) {
+    if (odd[0] | odd[1] | odd[2] | odd[3]) {   // what clean_values took out
+      const int s0 = max(0, cbase + it.r0 / a.rep + 1 - it.k0) / kStep;
+#pragma unroll
+      for (int u = 0; u < NI; ++u) {
+        const int i = u * kThreads + threadIdx.x, row = row_of(i), e = el_of(i);
+        const int last = row < it.nr ? cbase + (it.r0 + row) / a.rep : -1;
+        for (int k = it.k0 + s0 * kStep; k <= last; ++k) {
           const T* vt = reinterpret_cast<const T*>(
-                            vpool + (size_t)clamp_page(a.s, table[k / a.s.page]) * a.s.page_bytes) +
+                            vpool + (size_t)clamp_page(a.s, table[k >> shift]) * a.s.page_bytes) +
                         hoff + (k & (a.s.page - 1));
 #pragma unroll
           for (int d = 0; d < 4; ++d) {
             const float v = Elem<T>::load(vt + (size_t)(e + d) * a.s.page);
-            if (!(fabsf(v) < INFINITY)) acc[d] += v;
+            if (!(fabsf(v) < INFINITY)) acc[u][d] += v;
           }
         }
       }
-      M::store4(static_cast<T*>(a.o) + at * D + e, acc);
-      if (e == 0 && a.lse) a.lse[at] = ll == 0.f ? -INFINITY : mm * a.scale + logf(ll);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < NI; ++u) {
+    const int i = u * kThreads + threadIdx.x, row = row_of(i), e = el_of(i);
+    if constexpr (FINISH) {
+      if (row >= it.nr) continue;
+      const int rr = it.r0 + row, q = rr / a.rep;
+      const size_t at = ((size_t)it.seq * a.max_new + q) * a.hq + head * a.rep + (rr - q * a.rep);
+      M::store4(static_cast<T*>(a.o) + at * D + e, acc[u]);
+      if (e == 0 && a.lse) a.lse[at] = ll[u] == 0.f ? -INFINITY : mm[u] * a.scale + logf(ll[u]);
     } else {
       // e = 32 dt + 8 g + 4 half
       reinterpret_cast<float4*>(part_o<D>(a, head, it.part))[(e / 8) * 64 + (e / 4 % 2) * 32 + row] =
-          float4{acc[0], acc[1], acc[2], acc[3]};
-      if (e == 0) part_ml(a, head, it.part)[row] = float2{mm, ll};
+          float4{acc[u][0], acc[u][1], acc[u][2], acc[u][3]};
+      if (e == 0) part_ml(a, head, it.part)[row] = float2{mm[u], ll[u]};
     }
   }
 }
