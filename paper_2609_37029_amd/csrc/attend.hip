@@ -37,9 +37,10 @@ constexpr int kBlock = 32;           // rows of a block of partial results
 // run at once, and the keys whose work an item costs on top of its own (its start,
 // and writing and joining its part).
 struct Tile { int rows, unit, slots, cost; };
-__host__ __device__ inline Tile tile_of(const PagesShape& s) {
-  return s.dtype == LDR_BF16 ? Tile{256, 4 * kStage, 256, 384} : Tile{32, 128, 512, 192};
+__host__ __device__ constexpr Tile tile_of(bool bf16) {
+  return bf16 ? Tile{256, 4 * kStage, 256, 384} : Tile{32, 128, 512, 192};
 }
+__host__ __device__ inline Tile tile_of(const PagesShape& s) { return tile_of(s.dtype == LDR_BF16); }
 // Rounds of items over the workgroups that run at once, at most.
 constexpr int kMaxRounds = 4;
 
@@ -128,9 +129,9 @@ __device__ inline long block_scan(long v, long* sums, long* total) {
   return before + inc - v;
 }
 
-__device__ inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
+__device__ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
-__device__ inline int wave_sum(int v) {
+template <typename T> __device__ inline T wave_sum(T v) {
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
   return v;
@@ -143,6 +144,7 @@ __device__ inline int even_step(int len, int n, int unit) {
 
 // The plan, in one workgroup: thread b has sequence b; what looks at all
 // sequences for each goes by waves, a sequence at a time.
+template <bool BF16>
 __global__ void __launch_bounds__(kBook)
 attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t* groups,
                    uint8_t* ws, AttendWs w) {
@@ -161,7 +163,7 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   int32_t* map = reinterpret_cast<int32_t*>(ws + w.map);
   SeqInfo* info = reinterpret_cast<SeqInfo*>(ws + w.info);
   Item* items = reinterpret_cast<Item*>(ws + w.items);
-  const Tile tile = tile_of(s);
+  constexpr Tile tile = tile_of(BF16);   // divisions by its entries are shifts
 
   const int all = in ? clamp_rows(s, p.state[s.rows + b]) : 0;
   const int held = in ? min(max(p.state[s.open + b], 0), all) : 0;
@@ -238,8 +240,8 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   const int common_rows = in ? common[ld] * s.page / tile.unit * tile.unit : 0;
   const int share = in && members[b] > 1 && common_rows >= kMinShared ? common_rows : 0;
   const int gopen = in ? gopens[b] : 0;
-  const long R = (long)open * rep, Rg = share && ld == b ? (long)gopen * rep : 0;
-  const int ot = (int)ceil_div(R, tile.rows), gt = (int)ceil_div(Rg, tile.rows);
+  const int R = open * rep, Rg = share && ld == b ? gopen * rep : 0;    // below 2^28
+  const int ot = ceil_div(R, tile.rows), gt = ceil_div(Rg, tile.rows);
   int len = open ? tile_keys(rows, open, share, (ot - 1) * tile.rows, rep, tile.unit) : 0;
   if (len < kMinMain) len = 0;
   const int glen = Rg ? share : 0;
@@ -252,26 +254,24 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   // a chunk's; else it is near an even spread, and half a chunk at the end.
   {
     const float even = (float)work * s.hkv / tile.slots;
-    const int least = max((int)min(even / kMaxRounds + 1.f, 5e8f), tile.unit);
+    const int least = max((int)min(even / kMaxRounds + 1.f, 1e8f), tile.unit);
     float best = INFINITY;
     int chunk = 0;
     for (int t = wave; t < 4 * NW; t += NW) {
       // from `least` to 2 x kMaxRounds of it, in even ratios
       const float x = least * __builtin_amdgcn_exp2f(t * (3.2f / (4 * NW)));
-      const int c = (int)ceil_div((long)x, tile.unit) * tile.unit;
-      int n = 0;
+      const int c = ceil_div((int)x, tile.unit) * tile.unit;
+      const float per = __builtin_amdgcn_rcpf((float)c);
+      float n = 0.f;           // of chunks, nearly: for an estimate
       for (int i = lane; i < s.batch; i += 64) {
-        const int l = o_len[i], o = opens[i];
-        n += ((o * rep + tile.rows - 1) / tile.rows) * ((l + c - 1) / c);
+        n += ceil_div(opens[i] * rep, tile.rows) * ceilf(o_len[i] * per);
         if (lead[i] == i && shares[i])
-          n += ((gopens[i] * rep + tile.rows - 1) / tile.rows) * ((shares[i] + c - 1) / c);
+          n += ceil_div(gopens[i] * rep, tile.rows) * ceilf(shares[i] * per);
       }
-      n = wave_sum(n);
-      const float wgs = (float)n * s.hkv;
-      const float cost = wgs <= tile.slots
-                             ? (float)c + tile.cost
-                             : ((float)work * s.hkv + wgs * tile.cost) / tile.slots +
-                                   0.5f * (c + tile.cost);
+      const float wgs = wave_sum(n) * s.hkv;
+      const float cost = wgs <= tile.slots ? (float)c + tile.cost
+                                           : (even * tile.slots + wgs * tile.cost) / tile.slots +
+                                                 0.5f * (c + tile.cost);
       if (cost < best) { best = cost; chunk = c; }
     }
     if (lane == 0) { cand_cost[wave] = best; cand_chunk[wave] = chunk; }
@@ -283,7 +283,7 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   for (int i = 1; i < NW; ++i)
     if (cand_cost[i] < best) { best = cand_cost[i]; chunk = cand_chunk[i]; }
   const int oc = (len + chunk - 1) / chunk, gc = (glen + chunk - 1) / chunk;
-  const int ob = (int)ceil_div(R, kBlock), gb = (int)ceil_div(Rg, kBlock);
+  const int ob = ceil_div(R, kBlock), gb = ceil_div(Rg, kBlock);
   // the list: each sequence's own items, then its group's; and the blocks of parts
   long n_items = 0, n_part = 0;
   const long off = block_scan((long)ot * oc + (long)gt * gc, sums, &n_items);
@@ -306,7 +306,7 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
     if (share) {
       f.grp_part = g_part[ld];
       f.grp_chunks = g_chunks[ld];
-      f.grp_blocks = (int)ceil_div((long)gopen * rep, kBlock);
+      f.grp_blocks = ceil_div(gopen * rep, kBlock);
       f.grp_off = (qoffs[b] - qoffs[ld]) * rep;
     }
     info[b] = f;
@@ -1133,7 +1133,8 @@ size_t attend_workspace_bytes(const PagesShape& s, int hq, int max_new) {
 
 hipError_t launch_attend_plan(const PagesShape& s, const PagesPtrs& p, int hq, int max_new,
                               const int32_t* groups, void* ws, hipStream_t st) {
-  hipLaunchKernelGGL(attend_plan_kernel, dim3(1), dim3(kBook), 0, st, s, p, hq, max_new, groups,
+  hipLaunchKernelGGL(s.dtype == LDR_BF16 ? attend_plan_kernel<true> : attend_plan_kernel<false>,
+                     dim3(1), dim3(kBook), 0, st, s, p, hq, max_new, groups,
                      static_cast<uint8_t*>(ws), plan_ws(s, hq, max_new));
   return hipGetLastError();
 }
