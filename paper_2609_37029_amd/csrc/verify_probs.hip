@@ -125,31 +125,44 @@ __global__ void __launch_bounds__(kThreads) probs_sum_kernel(ProbsArgs a) {
   const int first = (blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)) * a.run;
   const int last = min(first + a.run, a.parts);
   constexpr int W = VEC ? 4 : 1;
-  for (int c = first; c < last; ++c) {
-    const int v0 = c * kPart + lane * W;
-    float p[kLane], q[kLane];
+  struct Chunk { float p[kLane], q[kLane]; };
+  auto load = [&](Chunk& x, int c) {
 #pragma unroll
     for (int k = 0; k < kLane; k += W) {
-      const int v = v0 + k * 64;
+      const int v = c * kPart + lane * W + k * 64;
       const bool in = v < a.V;
       if constexpr (VEC) {
         const float4 z{0.f, 0.f, 0.f, 0.f};
-        *reinterpret_cast<float4*>(p + k) = in ? *reinterpret_cast<const float4*>(w.p + v) : z;
-        *reinterpret_cast<float4*>(q + k) = in && w.q ? *reinterpret_cast<const float4*>(w.q + v) : z;
+        *reinterpret_cast<float4*>(x.p + k) = in ? *reinterpret_cast<const float4*>(w.p + v) : z;
+        *reinterpret_cast<float4*>(x.q + k) =
+            in && w.q ? *reinterpret_cast<const float4*>(w.q + v) : z;
       } else {
-        p[k] = in ? w.p[v] : 0.f;
-        q[k] = in && w.q ? w.q[v] : 0.f;
+        x.p[k] = in ? w.p[v] : 0.f;
+        x.q[k] = in && w.q ? w.q[v] : 0.f;
       }
     }
+  };
+  auto add = [&](const Chunk& x, int c) {
     double res = 0.0, tgt = 0.0;
 #pragma unroll
     for (int k = 0; k < kLane; ++k) {
-      tgt += positive(p[k]);
-      if (s.rejected) res += residual(w, p[k], q[k], v0 + k / W * W * 64 + k % W);
+      tgt += positive(x.p[k]);
+      if (s.rejected)
+        res += residual(w, x.p[k], x.q[k], c * kPart + lane * W + k / W * W * 64 + k % W);
     }
     res = wave_sum(res);
     tgt = wave_sum(tgt);
     if (lane == 0) a.part[(size_t)b * a.parts + c] = Part{res, tgt};
+  };
+  if (first >= last) return;
+  Chunk x, y;                      // the next part on its way while one is added up
+  load(x, first);
+  for (int c = first; c < last; c += 2) {
+    if (c + 1 < last) load(y, c + 1);
+    add(x, c);
+    if (c + 1 >= last) break;
+    if (c + 2 < last) load(x, c + 2);
+    add(y, c + 1);
   }
 }
 
