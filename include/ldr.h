@@ -284,7 +284,7 @@ void ldr_views_destroy(ldr_views* v);
  * one) is clamped where it is read. */
 typedef struct ldr_pages_config {
   int32_t n_layers;      /* layers in the pool                                */
-  int32_t n_kv_heads;
+  int32_t n_kv_heads;    /* n_layers * n_kv_heads <= 65535, each <= 1024      */
   int32_t head_dim;      /* 64 or 128                                         */
   int32_t page;          /* rows of a page: 32, 64, 128 or 256                */
   int32_t n_pages;       /* pages of the pool                                 */
@@ -322,8 +322,8 @@ int ldr_pages_reserve(ldr_pages* p, const int32_t* n_new, int32_t max_new, void*
 
 /* Writes the open rows of every sequence in layers [layer, layer + n_layers):
  * row r of K and V (r < min(open[b], max_new)) is the sequence's row
- * rows[b] - open[b] + r. max_new is the reserve's. With all layers these are the
- * K_new and V_new of ldr_views_update.
+ * rows[b] - open[b] + r. max_new is the reserve's, at most 2^28. With all
+ * layers these are the K_new and V_new of ldr_views_update.
  *   K, V  dev [batch][max_new][n_layers][n_kv_heads][head_dim] dtype */
 int ldr_pages_write(ldr_pages* p, int32_t layer, int32_t n_layers, const void* K, const void* V,
                     int32_t max_new, void* stream);
@@ -359,12 +359,13 @@ void ldr_pages_destroy(ldr_pages* p);
 
 /* Workspace bytes of ldr_attend_plan and of the ldr_attend calls that follow it
  * (0 for an invalid configuration or size: n_q_heads is a multiple of
- * n_kv_heads; batch * max_new * n_q_heads < 2^28). */
+ * n_kv_heads; batch * max_new * n_q_heads < 2^27). */
 size_t ldr_attend_workspace_bytes(const ldr_pages_config* cfg, int32_t n_q_heads,
                                   int32_t max_new);
 
 /* Plans the attention of the open rows over the cache as it is now; one plan
- * serves every layer, until a call on the handle changes the cache. Sequences
+ * serves every layer, until a call on the handle changes the cache or its state
+ * is put back (which ldr_attend does not notice). Sequences
  * with the same groups[b] >= 0 (a negative one: alone; NULL: the sequences whose
  * first page is the same one) read the pages that all of them have in common at
  * the front of their tables once, for all their rows together. Which sequences
@@ -591,7 +592,7 @@ int ldr_verify(const float* target_logits, const float* draft_logits, const floa
                int32_t* accepted, int32_t* next_token, int32_t* n_new, void* workspace,
                size_t workspace_bytes, void* stream);
 
-/* Workspace bytes ldr_verify_probs needs (0 on a non-positive size). */
+/* Workspace bytes ldr_verify_probs needs (0 on a size that it refuses). */
 size_t ldr_verify_probs_workspace_bytes(int32_t batch, int32_t block, int32_t vocab);
 
 /* Speculative verification (Eq. 1-2) from probabilities and random numbers that
@@ -619,8 +620,8 @@ size_t ldr_verify_probs_workspace_bytes(int32_t batch, int32_t block, int32_t vo
  *   accepted, next_token, n_new  dev int32 [batch], as ldr_verify's
  *   workspace    dev, ldr_verify_probs_workspace_bytes(batch, block, vocab)
  *                bytes, 16-byte aligned
- * LDR_EINVAL on a NULL pointer, a non-positive size, a vocab above 2^30 or a
- * short or misaligned workspace. */
+ * LDR_EINVAL on a NULL pointer, a non-positive size, a batch above 65535, a block
+ * or vocab above 2^30 or a short or misaligned workspace. */
 int ldr_verify_probs(const float* target_probs, const float* draft_probs,
                      const int32_t* draft_tokens, const int32_t* n_draft, const float* uniforms,
                      int32_t batch, int32_t block, int32_t vocab, int32_t* accepted,

@@ -655,7 +655,9 @@ int ldr_verify(const float* target_logits, const float* draft_logits, const floa
 }
 
 size_t ldr_verify_probs_workspace_bytes(int32_t batch, int32_t block, int32_t vocab) {
-  if (batch <= 0 || block <= 0 || vocab <= 0 || vocab > (1 << 30)) return 0;
+  if (batch <= 0 || batch > 65535 || block <= 0 || block > (1 << 30) || vocab <= 0 ||
+      vocab > (1 << 30))
+    return 0;
   return verify_probs_workspace_bytes(batch, block, vocab);
 }
 
@@ -667,10 +669,8 @@ int ldr_verify_probs(const float* target_probs, const float* draft_probs,
   if (!target_probs || !draft_tokens || !uniforms || !accepted || !next_token || !n_new ||
       !workspace)
     return LDR_EINVAL;
-  if (batch <= 0 || block <= 0 || vocab <= 0 || vocab > (1 << 30)) return LDR_EINVAL;
-  if (workspace_bytes < ldr_verify_probs_workspace_bytes(batch, block, vocab) ||
-      !aligned(workspace, 16))
-    return LDR_EINVAL;
+  const size_t need = ldr_verify_probs_workspace_bytes(batch, block, vocab);
+  if (!need || workspace_bytes < need || !aligned(workspace, 16)) return LDR_EINVAL;
   return launch_verify_probs(target_probs, draft_probs, draft_tokens, n_draft, uniforms, batch,
                              block, vocab, accepted, next_token, n_new, workspace,
                              static_cast<hipStream_t>(stream)) == hipSuccess

@@ -17,6 +17,7 @@ static bool make_pages_shape(const ldr_pages_config* c, PagesShape* s) {
   if (!c) return false;
   if (c->n_layers < 1 || c->n_layers > 1024 || c->n_kv_heads < 1 || c->n_kv_heads > 1024)
     return false;
+  if (c->n_layers * c->n_kv_heads > 65535) return false;   // a grid's second dimension
   if (c->head_dim != 64 && c->head_dim != 128) return false;
   if (c->page != 32 && c->page != 64 && c->page != 128 && c->page != 256) return false;
   if (c->n_pages < 1 || c->n_pages > (1 << 28)) return false;
@@ -43,7 +44,7 @@ static bool make_pages_shape(const ldr_pages_config* c, PagesShape* s) {
 
 static bool attend_sizes_ok(const PagesShape& s, int32_t hq, int32_t max_new) {
   return hq > 0 && hq % s.hkv == 0 && max_new > 0 &&
-         (int64_t)s.batch * max_new < (1 << 28) / (int64_t)hq;
+         (int64_t)s.batch * max_new < (1 << 27) / (int64_t)hq;
 }
 
 }  // namespace ldr
@@ -108,7 +109,7 @@ int ldr_pages_write(ldr_pages* p, int32_t layer, int32_t n_layers, const void* K
                     int32_t max_new, void* stream) {
   if (!p || layer < 0 || n_layers < 1 || layer >= p->s.layers || n_layers > p->s.layers - layer)
     return LDR_EINVAL;
-  if (max_new < 1 || max_new >= (1 << 30) || !K || !V || !aligned(K, 16) || !aligned(V, 16))
+  if (max_new < 1 || max_new > (1 << 28) || !K || !V || !aligned(K, 16) || !aligned(V, 16))
     return LDR_EINVAL;
   return done(launch_pages_write(p->s, p->p, layer, n_layers, K, V, max_new,
                                  static_cast<hipStream_t>(stream)));

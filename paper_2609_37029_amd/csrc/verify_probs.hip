@@ -262,9 +262,10 @@ hipError_t launch_verify_probs(const float* P, const float* Q, const int32_t* y,
                                int32_t* accepted, int32_t* token, int32_t* n_new, void* ws,
                                hipStream_t st) {
   const int parts = (V + kPart - 1) / kPart;
-  // each workgroup tests the candidates first: few workgroups a sequence, as long as
-  // all of them fill the GPU
-  const int run = max(1, min(8, (int)((long)parts * batch / 3072)));
+  // A wave's parts: its workgroup tests the candidates first, and its next part's
+  // loads need one before them; but 4096 waves, 4 a SIMD, come first. 64 sequences of
+  // 151936 tokens: 30.1 us with 2 parts a wave, 31.2 with 3, 32.9 with 4, 36 with 8.
+  const int run = max(1, min(8, (int)((long)parts * batch / 4096)));
   ProbsArgs a{P, Q, y, n_draft, u, batch, B, V, parts, run, static_cast<Part*>(ws), accepted, token,
               n_new};
   const bool vec = V % 4 == 0 && reinterpret_cast<uintptr_t>(P) % 16 == 0 &&

@@ -138,7 +138,7 @@ def _cfg(L, **kw):
 @pytest.mark.parametrize("bad", [
     dict(n_layers=0), dict(n_kv_heads=0), dict(head_dim=96), dict(page=48), dict(page=512),
     dict(n_pages=0), dict(batch=0), dict(batch=1025), dict(max_pages=0),
-    dict(max_pages=1 << 24), dict(dtype=2)])
+    dict(max_pages=1 << 24), dict(n_layers=256, n_kv_heads=256), dict(dtype=2)])
 def test_pages_config_refusals(L, bad):
     lib, c = L.lib(), ctypes.byref(_cfg(L, **bad))
     assert lib.ldr_pages_pool_bytes(c) == 0 and lib.ldr_pages_state_bytes(c) == 0
@@ -192,10 +192,11 @@ def test_verify_probs_host_refusals(L):
     assert need > 0
     for i in (0, 2, 4, 8, 9, 10, 11):
         assert lib.ldr_verify_probs(*good[:i], None, *good[i + 1:]) == L.LDR_EINVAL
-    for i, x in ((5, 0), (6, 0), (7, 0), (7, (1 << 30) + 1), (12, need - 1),
+    for i, x in ((5, 0), (5, 65536), (6, 0), (6, (1 << 30) + 1), (7, 0), (7, (1 << 30) + 1), (12, need - 1),
                  (11, ctypes.c_void_p((1 << 20) + 8))):
         assert lib.ldr_verify_probs(*good[:i], x, *good[i + 1:]) == L.LDR_EINVAL
-    for sizes in ((0, 4, 64), (2, 0, 64), (2, 4, 0), (2, 4, (1 << 30) + 1)):
+    for sizes in ((0, 4, 64), (65536, 4, 64), (2, 0, 64), (2, (1 << 30) + 1, 64), (2, 4, 0),
+                  (2, 4, (1 << 30) + 1)):
         assert lib.ldr_verify_probs_workspace_bytes(*sizes) == 0
 
 
