@@ -163,26 +163,13 @@ __device__ inline void copy_piece(const PagesShape& s, const PagesPtrs& p, int p
   }
 }
 
-// The copies that a reserve asked for, at most one page a sequence: of its rows
-// before the open ones, one workgroup per (head, layer, sequence). Whole pages would
-// be 7 times the bytes where 9 rows of 64 are used (64 forks of the Qwen3-8B cache).
+// The copies that a reserve asked for, at most one page a sequence: whole pages, so
+// that the copy holds what its original does behind the rows too.
 __global__ void __launch_bounds__(kThreads) pages_part_kernel(PagesShape s, PagesPtrs p) {
   const int b = blockIdx.z;
   const int from = p.state[s.pairs + 2 * b], to = p.state[s.pairs + 2 * b + 1];
   if (from < 0 || from >= s.n_pages || to < 0 || to >= s.n_pages) return;
-  const int part = max(p.state[s.rows + b] - p.state[s.open + b], 0) % s.page;
-  const size_t plane = (size_t)s.n_pages * s.page_bytes;
-  uint8_t* base = p.pool + 2 * blockIdx.y * plane + blockIdx.x * (s.page_bytes / s.hkv);
-  const uint4* in = reinterpret_cast<const uint4*>(base + (size_t)from * s.page_bytes);
-  uint4* out = reinterpret_cast<uint4*>(base + (size_t)to * s.page_bytes);
-  // K: `part` rows; V: as many columns, rounded up to 16 bytes, of head_dim rows
-  const int e = 16 / (int)s.el, width = (part + e - 1) / e, pitch = s.page / e;
-  const int nk = part * s.d / e, n = nk + s.d * width;
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const int j = i - nk;
-    const size_t at = j < 0 ? i : plane / 16 + j / width * pitch + j % width;
-    out[at] = in[at];
-  }
+  copy_piece(s, p, blockIdx.y, blockIdx.x, from, to);
 }
 
 // Open rows into their pages: one workgroup per (32 positions, layer and head,
@@ -386,8 +373,8 @@ hipError_t launch_pages_reserve(const PagesShape& s, const PagesPtrs& p, const i
   hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(kBook), 0, st, s, p, n_new, max_new);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(pages_part_kernel, dim3(s.hkv, s.layers, s.batch), dim3(kThreads), 0, st, s,
-                     p);
+  hipLaunchKernelGGL(pages_part_kernel, dim3(pieces_of(s), 2 * s.layers, s.batch), dim3(kThreads),
+                     0, st, s, p);
   return hipGetLastError();
 }
 

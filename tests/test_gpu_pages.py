@@ -190,3 +190,20 @@ def test_captured_round(gpu_lib):
         c.g.state.copy_(saved)
         c.check()
     assert c.g.status() == gpu_lib.LDR_OK
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_copied_page_is_whole(gpu_lib, dtype):
+    """A part-filled page that two sequences hold: who gets one of its own gets what
+    lies behind the rows too."""
+    c = Both(gpu_lib, 2, 3, 64, 64, 9, 3, 3, dtype)
+    g = c.g
+    g.pool.view(torch.uint8).random_(0, 120)          # finite in both types
+    c.append([70, 0, 5])
+    c.fork([0, 0, 2])
+    old, before = int(g.table[0, 1]), g.pool.clone()
+    g.reserve(i32([1, 1, 1]), 1)
+    a, b = int(g.table[0, 1]), int(g.table[1, 1])
+    assert a != b and a != old and b != old
+    for to in (a, b):
+        assert torch.equal(g.pool[:, :, to], before[:, :, old])
