@@ -28,8 +28,14 @@ constexpr int kWideThreads = 512;
 constexpr int kBook = 1024;          // threads of the plan's workgroup
 constexpr int kStep = 32;            // keys of a step; a page holds whole steps
 constexpr int kStage = 64;           // keys of a stage of the bf16 main kernel
-constexpr int kMinShared = 256;      // keys in common that are worth a segment of their own
-constexpr int kMinMain = 512;        // keys of a sequence's own that are worth items
+// Keys in common that are worth a segment of their own. 64 sequences with one row, 300
+// keys of their own and as many in common, two layers: 77 us with the segment and 88
+// without at 256 keys, 76 and 97 at 512.
+constexpr int kMinShared = 256;
+// Keys of a sequence's own that are worth items; fewer are left to the last kernel. 64
+// sequences as above with 32768 keys in common: 167 us, 181 if their 256 keys become
+// items; with 700 keys of their own 139 us, 154 if they do not.
+constexpr int kMinMain = 512;
 constexpr int kBlock = 32;           // rows of a block of partial results
 
 // Tiles of a dtype's main kernel: rows of an item, the keys that an item's are a
@@ -41,8 +47,9 @@ __host__ __device__ constexpr Tile tile_of(bool bf16) {
   return bf16 ? Tile{256, 4 * kStage, 256, 384} : Tile{32, 128, 512, 192};
 }
 __host__ __device__ inline Tile tile_of(const PagesShape& s) { return tile_of(s.dtype == LDR_BF16); }
-// Rounds of items over the workgroups that run at once, at most.
-constexpr int kMaxRounds = 4;
+// Rounds of items over the workgroups that run at once, at most (4 took 2% longer: the
+// grid is sized for as many, and most of it ends at once).
+constexpr int kMaxRounds = 2;
 
 // One unit of work: rows r0 .. r0 + nr of a segment over keys k0 .. k1 of
 // sequence seq. Row r belongs to the segment's query r / rep, entry q0 + r / rep
@@ -839,7 +846,8 @@ attend_wide_kernel(AttendArgs a) {
   const size_t page_el = a.s.page_bytes / 2;
 
   // Up to 128 rows: both groups take the same rows, each 32 of a stage's keys,
-  // and join at the end. The lane's query; columns behind the last row repeat it.
+  // and join at the end (16 sequences with 68 rows over 8192 keys of their own, two
+  // layers: 232 us; 239 if half of the waves are idle). The lane's query; columns behind the last row repeat it.
   const bool split = it.nr <= NW / 2 * kBlock;
   const int block = split ? wave % (NW / 2) : wave;
   const bool active = block * kBlock < it.nr;
