@@ -25,21 +25,21 @@ __device__ inline int pages_of(const PagesShape& s, int rows) { return (rows + s
 
 // Exclusive prefix sum of one value per thread of a bookkeeping workgroup, and
 // the total. `sums`: kBook / 64 words of LDS.
-__device__ inline int block_scan(int v, int* sums, int* total) {
+template <typename T> __device__ inline T block_scan(T v, T* sums, T* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int inc = v;
+  T inc = v;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
-    const int o = __shfl_up(inc, off);
+    const T o = __shfl_up(inc, off);
     if (lane >= off) inc += o;
   }
   __syncthreads();   // the last call's readers are done
   if (lane == 63) sums[wave] = inc;
   __syncthreads();
-  int before = 0, all = 0;
+  T before = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < kBook / 64; ++w) {
-    const int x = sums[w];
+    const T x = sums[w];
     before += w < wave ? x : 0;
     all += x;
   }
@@ -59,6 +59,7 @@ __global__ void pages_clear_flags_kernel(PagesPtrs p) { p.state[kPagesFlags] = 0
 // which of them a sequence gets, its copy of a shared partial page first.
 __global__ void __launch_bounds__(kBook)
 pages_reserve_kernel(PagesShape s, PagesPtrs p, const int32_t* n_new, int max_new) {
+  __shared__ long needs[kBook / 64];
   __shared__ int sums[kBook / 64], start[kBook], first_slot[kBook];
   __shared__ uint8_t granted[kBook];
   const int b = threadIdx.x;
@@ -86,8 +87,10 @@ pages_reserve_kernel(PagesShape s, PagesPtrs p, const int32_t* n_new, int max_ne
       need = pages_of(s, rows + n) - first;
     }
   }
-  int want = 0;
-  const int at = block_scan(need, sums, &want);
+  long all = 0;     // of all sequences: may be more than an int holds
+  const long before = block_scan((long)need, needs, &all);
+  const int want = (int)min(all, (long)s.n_pages);
+  const int at = (int)min(before, (long)s.n_pages);
   start[b] = at;
   first_slot[b] = first;
   // the first `want` free pages (fewer if there are not as many)

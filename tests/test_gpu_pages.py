@@ -207,3 +207,19 @@ def test_a_copied_page_is_whole(gpu_lib, dtype):
     assert a != b and a != old and b != old
     for to in (a, b):
         assert torch.equal(g.pool[:, :, to], before[:, :, old])
+
+
+def test_wants_of_more_than_an_int(gpu_lib):
+    """66 sequences that each want all of a table of 2^25 - 1 pages, 2^31 and more
+    together, of a pool of 4: none of them gets any, whatever is behind it."""
+    b, most = 66, (1 << 25) - 1
+    p = gpu_lib.Pages(1, 1, 64, 32, 4, b, most, BF).init()
+    n = i32([most * 32] * (b - 1) + [1])
+    p.reserve(n, most * 32)
+    assert p.status(clear=True) == gpu_lib.LDR_EPAGES
+    assert not p.rows.any() and not p.open.any() and not p.refs.any()
+    n[:-1] = 0
+    p.reserve(n, 1)
+    assert p.status() == gpu_lib.LDR_OK
+    assert p.rows.tolist() == [0] * (b - 1) + [1] and p.refs.tolist() == [1, 0, 0, 0]
+    assert int(p.table[b - 1, 0]) == 0
