@@ -174,7 +174,7 @@ int ldr_attend(const ldr_pages* p, int32_t layer, const void* q, int64_t q_strid
   if (!q || !o || !aligned(q, 16) || !aligned(o, 16) || !aligned(lse, 4)) return LDR_EINVAL;
   if (q_stride < (int64_t)n_q_heads * p->s.d || q_stride % (16 / (int64_t)p->s.el))
     return LDR_EINVAL;
-  if (!(scale > 0.f) || std::isinf(scale)) return LDR_EINVAL;
+  if (!std::isnormal(scale) || scale < 0.f) return LDR_EINVAL;
   if (!workspace || !aligned(workspace, kAlign) ||
       workspace_bytes < attend_workspace_bytes(p->s, n_q_heads, max_new))
     return LDR_EINVAL;

@@ -5,6 +5,11 @@
 // whose order could change a result: free pages go to the sequences lowest id
 // first. References are counted with atomic adds, which commute. What moves
 // bytes (rows into pages, whole pages) runs over the GPU and is bound by HBM.
+//
+// Measured, Qwen3-8B heads, five layers, pages of 64: reserve 5 us, keep 2, fork 5 (64
+// sequences); rows of 64 x 17 tokens 16 us (45 MB in and out), of 16 x 17 7 us; copies of
+// 64 pages 26 us (84 MB written, the source in cache); compaction of half the pages of 32
+// x 4096 rows 256 us (1.2 GB, 4.7 TB/s).
 #include "ldr_internal.h"
 
 namespace ldr {
@@ -179,7 +184,8 @@ __global__ void __launch_bounds__(kThreads) pages_part_kernel(PagesShape s, Page
 // sequence), on two pages at most. K rows are copied; V is transposed through LDS
 // and stored by runs of 16 bytes of one dimension. Tiles begin at multiples of such
 // a run, so that no two workgroups write to one; the first and the last run keep
-// their other rows, which nobody else writes (the page is the sequence's own).
+// their other rows, which nobody else writes (the page is the sequence's own). Stores
+// of single values, dimension by dimension, took 10 and 26 us instead of 7 and 16.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 pages_write_kernel(PagesShape s, PagesPtrs p, int layer0, int n_layers, const T* K, const T* V,

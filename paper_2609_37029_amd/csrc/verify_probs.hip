@@ -12,7 +12,9 @@
 //
 // Bound by reading one target and one draft row a sequence, once, and at small
 // batches by the latency of the chain: tokens, gathers, rows, sums, second launch,
-// part.
+// part. 64 sequences of 151936 tokens: sums 17 us (78 MB, 4.5 TB/s), draw 12 us; one: 5
+// and 11. With a workgroup a part of 4096, and without the next part's loads under way,
+// 64 took 56 and 41 us.
 #include "ldr_internal.h"
 
 namespace ldr {

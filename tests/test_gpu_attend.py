@@ -149,7 +149,7 @@ def test_strided_queries_and_streams(gpu_lib):
         gpu_lib.attend(c.g.plan(8, 5), 0, q.float())
     with pytest.raises(gpu_lib.LdrError):
         gpu_lib.attend(c.g.plan(8, 5), 1, q)    # no such layer
-    for scale in (0.0, -1.0, float("nan"), float("inf")):
+    for scale in (0.0, -1.0, 1e-40, float("nan"), float("inf")):
         with pytest.raises(gpu_lib.LdrError):
             gpu_lib.attend(c.g.plan(8, 5), 0, q, scale=scale)
 
@@ -225,3 +225,26 @@ def test_same_bits_every_time(gpu_lib):
         out = gpu_lib.attend(c.g.plan(8, 17), 0, q)
         torch.cuda.synchronize()
         assert torch.equal(out, o)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("hq,new", [(1, 1), (2, 1), (3, 1), (1, 7), (8, 1), (4, 5), (8, 4)])
+def test_few_rows_of_many_parts(gpu_lib, dtype, d, hq, new):
+    """1 to 32 rows over enough keys for some twenty parts each, which are joined
+    side by side; one sequence has none, one a single part."""
+    c = Both(gpu_lib, 1, 1, d, 64, 200, 3, 90, dtype, seed=hq)
+    c.append([5000, 100, 600])
+    c.append([new, new, new])
+    _run(gpu_lib, c, hq, new)
+
+
+def test_a_thousand_sequences(gpu_lib):
+    """As many sequences as a cache takes, in groups of one prompt, strangers and empty
+    ones between them."""
+    b = 1024
+    c = Both(gpu_lib, 1, 1, 64, 32, 4096, b, 24, F32, seed=9)
+    src = np.array([i % 8 if i % 7 < 5 else i for i in range(b)])
+    c.append([[300, 520, 33, 700, 31, 256, 290, 0][i] if i < 8 else 0 for i in range(b)], 700)
+    c.fork(src)
+    c.append([i % 3 for i in range(b)], 2)
+    _run(gpu_lib, c, 2, 2)
