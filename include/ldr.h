@@ -606,8 +606,9 @@ size_t ldr_verify_probs_workspace_bytes(int32_t batch, int32_t block, int32_t vo
  * after n_draft[b] acceptances one of w = p_{n_draft[b] + 1}, by inverting the
  * cumulative sum: the first token with w_v > 0 and C_v > u_block C_{vocab - 1},
  * C_v = w_0 + .. + w_v; where there is none (u_block >= 1, NaN) the last token
- * with w_v > 0, and 0 for a row without one. Differences and sums are fp64, so
- * that a draw does not depend on their order; entries of w that are not finite
+ * with w_v > 0, and 0 for a row without one. Differences and sums are fp64: their
+ * order matters only where u_block C_{vocab - 1} meets a C_v to within 2^-35;
+ * entries of w that are not finite
  * and above 0 count as 0. Probabilities need not sum to 1.
  *   target_probs dev fp32 [batch][block + 1][vocab]
  *   draft_probs  dev fp32 [batch][block][vocab]; NULL for proposals without a

@@ -7,7 +7,7 @@
 // part in which the cumulative sum passes u C and the token inside it.
 //
 // fp64: differences of fp32 numbers and sums of 150 thousand of them lose nothing
-// that a draw could see, so the token does not depend on how the sum is cut up.
+// that a draw could see: how the sum is cut up matters within 2^-35 of a border only.
 // The test u q < p compares a 48-bit product exactly.
 //
 // Bound by reading one target and one draft row a sequence, once, and at small
