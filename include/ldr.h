@@ -607,9 +607,8 @@ size_t ldr_verify_probs_workspace_bytes(int32_t batch, int32_t block, int32_t vo
  * cumulative sum: the first token with w_v > 0 and C_v > u_block C_{vocab - 1},
  * C_v = w_0 + .. + w_v; where there is none (u_block >= 1, NaN) the last token
  * with w_v > 0, and 0 for a row without one. Differences and sums are fp64: their
- * order matters only where u_block C_{vocab - 1} meets a C_v to within 2^-35;
- * entries of w that are not finite
- * and above 0 count as 0. Probabilities need not sum to 1.
+ * order matters only where u_block C_{vocab - 1} meets a C_v to within their
+ * rounding. Entries of w that are not finite and above 0 count as 0. Probabilities need not sum to 1.
  *   target_probs dev fp32 [batch][block + 1][vocab]
  *   draft_probs  dev fp32 [batch][block][vocab]; NULL for proposals without a
  *                distribution (drafted greedily or looked up): q_i is 1 at y_i

@@ -7,7 +7,7 @@
 // part in which the cumulative sum passes u C and the token inside it.
 //
 // fp64: differences of fp32 numbers and sums of 150 thousand of them lose nothing
-// that a draw could see: how the sum is cut up matters within 2^-35 of a border only.
+// that a draw could see: how the sum is cut up matters within their rounding of a border only.
 // The test u q < p compares a 48-bit product exactly.
 //
 // Bound by reading one target and one draft row a sequence, once, and at small
@@ -21,6 +21,7 @@ namespace ldr {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
 constexpr int kPart = 1024;            // tokens of a part
 constexpr int kEach = kPart / kThreads;    // tokens of a part a thread draws from
 constexpr int kLane = kPart / 64;          // and a lane sums
@@ -48,9 +49,8 @@ __device__ inline double positive(double w) {
 struct Stop { int r; bool rejected; };
 
 __device__ Stop find_stop(const ProbsArgs& a, int b) {
-  __shared__ int first;
-  if (threadIdx.x == 0) first = a.B;
-  __syncthreads();
+  __shared__ int firsts[kWaves];
+  int first = a.B;
   const int n = a.n ? min(max(a.n[b], 0), a.B) : a.B;
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const int y = a.y[(size_t)b * a.B + i];
@@ -61,11 +61,16 @@ __device__ Stop find_stop(const ProbsArgs& a, int b) {
       ok = (double)a.u[(size_t)b * (a.B + 1) + i] * (double)q < (double)p;
     }
     if (!ok) {
-      atomicMin(&first, i);
+      first = i;
       break;
     }
   }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) first = min(first, __shfl_xor(first, off));
+  if ((threadIdx.x & 63) == 0) firsts[threadIdx.x >> 6] = first;
   __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) first = min(first, firsts[k]);
   const int r = min(first, n);
   return Stop{r, r < n};
 }
@@ -106,12 +111,31 @@ __device__ inline double block_scan(double v, double* sums, double* total) {
   __syncthreads();
   double before = 0.0, all = 0.0;
 #pragma unroll
-  for (int k = 0; k < kThreads / 64; ++k) {
+  for (int k = 0; k < kWaves; ++k) {
     before += k < wave ? sums[k] : 0.0;
     all += sums[k];
   }
   *total = all;
   return before + inc;
+}
+
+// A place that a thread found (-1: none), with what came before it.
+struct Found { int at; double before; };
+// The first of the threads that found one, or the last. By ballots: minima and maxima in
+// LDS, lane by lane, took 8 of the 11 us of the draw.
+template <bool LAST> __device__ inline Found pick(Found f, Found* found) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t have = __ballot(f.at >= 0);
+  if (have ? lane == (LAST ? 63 - __builtin_clzll(have) : __builtin_ctzll(have)) : lane == 0)
+    found[wave] = f;
+  __syncthreads();
+  Found r = found[LAST ? kWaves - 1 : 0];
+#pragma unroll
+  for (int i = 1; i < kWaves; ++i) {
+    const Found o = found[LAST ? kWaves - 1 - i : i];
+    if (r.at < 0) r = o;
+  }
+  return r;
 }
 
 // VEC: rows start on 16 bytes and V is a multiple of 4.
@@ -124,7 +148,7 @@ __global__ void __launch_bounds__(kThreads) probs_sum_kernel(ProbsArgs a) {
     a.n_new[b] = s.r + 1;
   }
   const Row w = row_of(a, b, s);
-  const int first = (blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)) * a.run;
+  const int first = (blockIdx.x * kWaves + (threadIdx.x >> 6)) * a.run;
   const int last = min(first + a.run, a.parts);
   constexpr int W = VEC ? 4 : 1;
   struct Chunk { float p[kLane], q[kLane]; };
@@ -170,9 +194,8 @@ __global__ void __launch_bounds__(kThreads) probs_sum_kernel(ProbsArgs a) {
 
 template <bool VEC>
 __global__ void __launch_bounds__(kThreads) probs_draw_kernel(ProbsArgs a) {
-  __shared__ double sums[kThreads / 64];
-  __shared__ double before[2];        // of the part that holds the draw, and of the last one
-  __shared__ int part, last_part, found, last;
+  __shared__ double sums[kWaves];
+  __shared__ Found hits[kWaves], lasts[kWaves], hit_tokens[kWaves], last_tokens[kWaves];
   const int b = blockIdx.x, tid = threadIdx.x;
   const int r = a.accepted[b];
   const int n = a.n ? min(max(a.n[b], 0), a.B) : a.B;
@@ -180,7 +203,6 @@ __global__ void __launch_bounds__(kThreads) probs_draw_kernel(ProbsArgs a) {
   const Stop s{r, r < n};
   const Row w = row_of(a, b, s);
   const Part* pt = a.part + (size_t)b * a.parts;
-  if (tid == 0) { part = a.parts; last_part = -1; found = a.V; last = -1; }
   // a run of consecutive parts a thread
   const int each = (a.parts + kThreads - 1) / kThreads;
   const int c0 = min(tid * each, a.parts), c1 = min(c0 + each, a.parts);
@@ -190,25 +212,18 @@ __global__ void __launch_bounds__(kThreads) probs_draw_kernel(ProbsArgs a) {
   double total = 0.0;
   double cum = block_scan(use ? res : tgt, sums, &total) - (use ? res : tgt);
   const double t = u * total;
-  int at = -1, final = -1;
-  double at_before = 0.0, final_before = 0.0;
+  Found at{-1, 0.0}, final{-1, 0.0};
   for (int c = c0; c < c1; ++c) {
     const double x = use ? pt[c].res : pt[c].tgt;
     if (x > 0.0) {
-      if (at < 0 && cum + x > t) { at = c; at_before = cum; }
-      final = c;
-      final_before = cum;
+      if (at.at < 0 && cum + x > t) at = Found{c, cum};
+      final = Found{c, cum};
     }
     cum += x;
   }
-  if (at >= 0) atomicMin(&part, at);
-  if (final >= 0) atomicMax(&last_part, final);
-  __syncthreads();
-  if (at >= 0 && part == at) before[0] = at_before;
-  if (final >= 0 && last_part == final) before[1] = final_before;
-  __syncthreads();
-  const bool hit_part = part < a.parts;
-  const int c = hit_part ? part : last_part;
+  const Found hit_part = pick<false>(at, hits), last_part = pick<true>(final, lasts);
+  const Found in = hit_part.at >= 0 ? hit_part : last_part;
+  const int c = in.at;
   if (c < 0) {   // no entry above 0
     if (tid == 0) a.token[b] = 0;
     return;
@@ -232,25 +247,23 @@ __global__ void __launch_bounds__(kThreads) probs_draw_kernel(ProbsArgs a) {
     }
   }
   double x[kEach], sum = 0.0;
-  int end = -1;
+  Found end{-1, 0.0}, hit{-1, 0.0};
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
     x[k] = use ? residual(w, p[k], q[k], v0 + k) : positive(p[k]);   // 0 behind the row
-    if (x[k] > 0.0) end = v0 + k;
+    if (x[k] > 0.0) end.at = v0 + k;
     sum += x[k];
   }
   double all = 0.0;
-  double run = before[hit_part ? 0 : 1] + block_scan(sum, sums, &all) - sum;
-  int hit = a.V;
+  double run = in.before + block_scan(sum, sums, &all) - sum;
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
     run += x[k];
-    if (hit == a.V && x[k] > 0.0 && run > t) hit = v0 + k;
+    if (hit.at < 0 && x[k] > 0.0 && run > t) hit.at = v0 + k;
   }
-  if (hit < a.V) atomicMin(&found, hit);
-  if (end >= 0) atomicMax(&last, end);
-  __syncthreads();
-  if (tid == 0) a.token[b] = found < a.V ? found : last;
+  hit = pick<false>(hit, hit_tokens);
+  end = pick<true>(end, last_tokens);
+  if (tid == 0) a.token[b] = hit.at >= 0 ? hit.at : end.at;
 }
 
 }  // namespace
@@ -272,7 +285,7 @@ hipError_t launch_verify_probs(const float* P, const float* Q, const int32_t* y,
               n_new};
   const bool vec = V % 4 == 0 && reinterpret_cast<uintptr_t>(P) % 16 == 0 &&
                    reinterpret_cast<uintptr_t>(Q) % 16 == 0;
-  const int wg = run * (kThreads / 64);    // parts of a workgroup
+  const int wg = run * kWaves;    // parts of a workgroup
   const dim3 grid((parts + wg - 1) / wg, batch);
   if (vec) hipLaunchKernelGGL(probs_sum_kernel<true>, grid, dim3(kThreads), 0, st, a);
   else hipLaunchKernelGGL(probs_sum_kernel<false>, grid, dim3(kThreads), 0, st, a);
