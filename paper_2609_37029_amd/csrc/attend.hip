@@ -133,8 +133,7 @@ __device__ inline long block_scan(long v, long* sums, long* total) {
   if (lane == 63) sums[wave] = inc;
   __syncthreads();
   long before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kBook / 64; ++w) {
+  for (int w = 0; w < (int)blockDim.x / 64; ++w) {
     before += w < wave ? sums[w] : 0;
     all += sums[w];
   }
@@ -156,22 +155,23 @@ __device__ inline int even_step(int len, int n, int unit) {
 }
 
 // The plan, in one workgroup: thread b has sequence b; what looks at all
-// sequences for each goes by waves, a sequence at a time. 10 us for one sequence, 22 for
-// 64 with 512 pages in common (a wave compares the tables of four, one behind the other;
-// four at once took as long): once for all layers.
+// sequences for each goes by waves, a sequence at a time. 7.5 us for one sequence, 21 for
+// 64 with 512 pages in common (their tables, 128 KB, through one compute unit): once
+// for all layers.
 template <bool BF16>
 __global__ void __launch_bounds__(kBook)
 attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t* groups,
                    uint8_t* ws, AttendWs w) {
-  constexpr int NW = kBook / 64;
-  __shared__ long sums[NW];
+  constexpr int kMost = kBook / 64;
+  __shared__ long sums[kMost];
   __shared__ int label[kBook], lead[kBook], opens[kBook], fulls[kBook], common[kBook];
   __shared__ int qoffs[kBook], members[kBook], gopens[kBook];
   __shared__ int i_off[kBook], o_chunks[kBook], g_chunks[kBook], o_part[kBook], g_part[kBook];
   __shared__ int o_len[kBook], shares[kBook], ends[kBook];
-  __shared__ float cand_cost[NW];
-  __shared__ int cand_chunk[NW];
+  __shared__ float4 cuts[kBook];           // tiles and keys, own and shared
+  __shared__ float works[kMost], counts[kMost][64];
   const int b = threadIdx.x, lane = b & 63, wave = b >> 6, rep = hq / s.hkv;
+  const int NW = blockDim.x / 64;
   const bool in = b < s.batch;
   const int32_t* table = p.state + s.table;
   Header* hd = reinterpret_cast<Header*>(ws);
@@ -209,7 +209,9 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   }
   __syncthreads();
   // row map: the sequences of a group behind one another; pages in common with
-  // the first of the group, many loads at a time
+  // the first of the group, many loads at a time, those of the first once
+  constexpr int U = 8;
+  int y[U], y_of = -1, y_at = 0;
   for (int c = wave; c < s.batch; c += NW) {
     const int ld = lead[c];
     int before = 0, sum = 0;
@@ -228,21 +230,23 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
     const int lim = min(fulls[c], fulls[ld]);
     const int32_t* tc = table + (size_t)c * s.max_pages;
     const int32_t* tl = table + (size_t)ld * s.max_pages;
-    constexpr int U = 8;
     int same = lim;
     for (int j = 0; j < lim; j += 64 * U) {
-      int x[U], y[U];
+      int x[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int k = min(j + u * 64 + lane, lim - 1);
-        x[u] = tc[k];
-        y[u] = tl[k];
+      for (int u = 0; u < U; ++u) x[u] = tc[min(j + u * 64 + lane, lim - 1)];
+      if (y_of != ld || y_at != j) {
+        y_of = ld;
+        y_at = j;
+#pragma unroll
+        for (int u = 0; u < U; ++u) y[u] = tl[min(j + u * 64 + lane, fulls[ld] - 1)];
       }
       int at = lim;
 #pragma unroll
       for (int u = U - 1; u >= 0; --u) {
-        const uint64_t diff = __ballot(x[u] != y[u]);
-        if (diff) at = min(j + u * 64 + (int)__builtin_ctzll(diff), lim);
+        const int k = j + u * 64 + lane;
+        const uint64_t diff = __ballot(k < lim && x[u] != y[u]);
+        if (diff) at = j + u * 64 + (int)__builtin_ctzll(diff);
       }
       if (at < lim) { same = at; break; }
     }
@@ -263,46 +267,50 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   o_len[b] = len;
   shares[b] = share;
   ends[b] = rows;
-  long work = 0;
-  block_scan((long)ot * len + (long)gt * glen, sums, &work);
-  // The chunk: each wave tries some lengths. With slots for all items the time is
-  // a chunk's; else it is near an even spread, and half a chunk at the end.
-  {
-    const float even = (float)work * s.hkv / tile.slots;
-    const int least = max((int)min(even / kMaxRounds + 1.f, 1e8f), tile.unit);
-    float best = INFINITY;
-    int chunk = 0;
-    for (int t = wave; t < 4 * NW; t += NW) {
-      // from `least` to 2 x kMaxRounds of it, in even ratios
-      const float x = least * __builtin_amdgcn_exp2f(t * (3.2f / (4 * NW)));
-      const int c = ceil_div((int)x, tile.unit) * tile.unit;
-      const float per = __builtin_amdgcn_rcpf((float)c);
-      float n = 0.f;           // of chunks, nearly: for an estimate
-      for (int i = lane; i < s.batch; i += 64) {
-        n += ceil_div(opens[i] * rep, tile.rows) * ceilf(o_len[i] * per);
-        if (lead[i] == i && shares[i])
-          n += ceil_div(gopens[i] * rep, tile.rows) * ceilf(shares[i] * per);
-      }
-      const float wgs = wave_sum(n) * s.hkv;
-      const float cost = wgs <= tile.slots ? (float)c + tile.cost
-                                           : (even * tile.slots + wgs * tile.cost) / tile.slots +
-                                                 0.5f * (c + tile.cost);
-      if (cost < best) { best = cost; chunk = c; }
-    }
-    if (lane == 0) { cand_cost[wave] = best; cand_chunk[wave] = chunk; }
-  }
+  cuts[b] = float4{(float)ot, (float)len, (float)gt, (float)glen};
+  const float mine = wave_sum((float)ot * len + (float)gt * glen);
+  if (lane == 0) works[wave] = mine;
   __syncthreads();
-  int chunk = cand_chunk[0];
-  float best = cand_cost[0];
+  // The chunk: a lane has a length, a wave some of the sequences. With slots for all
+  // items the time is a chunk's; else it is near an even spread, and half a chunk at the
+  // end.
+  float work = 0.f;
+  for (int w = 0; w < NW; ++w) work += works[w];
+  const float even = work * s.hkv / tile.slots;
+  const int least = max((int)min(even / kMaxRounds + 1.f, 1e8f), tile.unit);
+  // from `least` to 4.5 x kMaxRounds of it, in even ratios
+  const float x = least * __builtin_amdgcn_exp2f(lane * (3.2f / 64));
+  int chunk = ceil_div((int)x, tile.unit) * tile.unit;
+  {
+    const float per = __builtin_amdgcn_rcpf((float)chunk);
+    float n = 0.f;           // of chunks, nearly: for an estimate
+    for (int i = wave; i < s.batch; i += NW) {
+      const float4 c = cuts[i];
+      n += c.x * ceilf(c.y * per) + c.z * ceilf(c.w * per);
+    }
+    counts[wave][lane] = n;
+    __syncthreads();
+    n = 0.f;
+    for (int w = 0; w < NW; ++w) n += counts[w][lane];
+    const float wgs = n * s.hkv;
+    float cost = wgs <= tile.slots ? (float)chunk + tile.cost
+                                   : (even * tile.slots + wgs * tile.cost) / tile.slots +
+                                         0.5f * (chunk + tile.cost);
 #pragma unroll
-  for (int i = 1; i < NW; ++i)
-    if (cand_cost[i] < best) { best = cand_cost[i]; chunk = cand_chunk[i]; }
+    for (int off = 32; off >= 1; off >>= 1) {
+      const float oc = __shfl_xor(cost, off);
+      const int ch = __shfl_xor(chunk, off);
+      if (oc < cost || (oc == cost && ch < chunk)) { cost = oc; chunk = ch; }
+    }
+  }
   const int oc = (len + chunk - 1) / chunk, gc = (glen + chunk - 1) / chunk;
   const int ob = ceil_div(R, kBlock), gb = ceil_div(Rg, kBlock);
   // the list: each sequence's own items, then its group's; and the blocks of parts
-  long n_items = 0, n_part = 0;
-  const long off = block_scan((long)ot * oc + (long)gt * gc, sums, &n_items);
-  const long part = block_scan((long)oc * ob + (long)gc * gb, sums, &n_part);
+  // both counts in one scan: below 2^31 each, by the bound on the chunk
+  long both = 0;
+  const long at = block_scan((long)(ot * oc + gt * gc) << 32 | (long)(oc * ob + gc * gb), sums, &both);
+  long n_items = both >> 32, n_part = both & 0xffffffff;
+  const long off = at >> 32, part = at & 0xffffffff;
   i_off[b] = (int)off;
   o_chunks[b] = oc; g_chunks[b] = gc;
   o_part[b] = (int)part;
@@ -336,7 +344,7 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   }
   for (int c = wave; c < s.batch; c += NW)
     for (int i = lane; i < opens[c]; i += 64) map[qoffs[c] + i] = c * max_new + i;
-  for (int t = b; t < (int)n_items; t += kBook) {
+  for (int t = b; t < (int)n_items; t += blockDim.x) {
     int lo = 0, hi = s.batch - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -1152,8 +1160,11 @@ size_t attend_workspace_bytes(const PagesShape& s, int hq, int max_new) {
 
 hipError_t launch_attend_plan(const PagesShape& s, const PagesPtrs& p, int hq, int max_new,
                               const int32_t* groups, void* ws, hipStream_t st) {
+  // a wave a sequence: four waves share a SIMD, so that 16 make every step four times as
+  // long (one sequence over 2048 keys, all launches: 20.9 us, 22.5 with 16)
+  const int waves = min(max(s.batch, 4), kBook / 64);
   hipLaunchKernelGGL(s.dtype == LDR_BF16 ? attend_plan_kernel<true> : attend_plan_kernel<false>,
-                     dim3(1), dim3(kBook), 0, st, s, p, hq, max_new, groups,
+                     dim3(1), dim3(64 * waves), 0, st, s, p, hq, max_new, groups,
                      static_cast<uint8_t*>(ws), plan_ws(s, hq, max_new));
   return hipGetLastError();
 }

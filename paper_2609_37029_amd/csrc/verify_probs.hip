@@ -12,8 +12,8 @@
 //
 // Bound by reading one target and one draft row a sequence, once, and at small
 // batches by the latency of the chain: tokens, gathers, rows, sums, second launch,
-// part. 64 sequences of 151936 tokens: sums 17 us (78 MB, 4.5 TB/s), draw 12 us; one: 5
-// and 11. With a workgroup a part of 4096, and without the next part's loads under way,
+// part. 64 sequences of 151936 tokens: sums 17 us (78 MB, 4.5 TB/s), draw 5 us; one: 5
+// and 4. With a workgroup a part of 4096, and without the next part's loads under way,
 // 64 took 56 and 41 us.
 #include "ldr_internal.h"
 
