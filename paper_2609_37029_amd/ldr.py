@@ -185,10 +185,15 @@ def _stream(stream=None):
 
 def _take(t: torch.Tensor, shape, dtype, device, name: str):
     """Refuses a tensor that the library would read as something else."""
-    if (tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device
+    if (t.shape != shape or t.dtype is not dtype or t.device != device
             or not t.is_contiguous()):
         raise LdrError(LDR_EINVAL, f"{name} of {tuple(t.shape)} {t.dtype} on {t.device}, needed "
                                    f"contiguous {tuple(shape)} {dtype} on {device}")
+
+
+def _on_gpu(device, what: str):
+    if device.type != "cuda":
+        raise LdrError(LDR_EINVAL, f"{what} on {device}")
 
 
 def _on(stream):
@@ -642,6 +647,7 @@ class Pages:
 
     def init(self):
         """ldr_pages_init: an empty cache (the pool is not written)."""
+        _on_gpu(self.device, "Pages.init")
         self.close()
         _check(_lib().ldr_pages_init(ctypes.byref(self._h), ctypes.byref(self.cfg),
                                      _ptr(self.pool), _ptr(self.state), _stream(self._stream)),
@@ -783,6 +789,8 @@ def verify_probs(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor]
     probabilities [batch][B][V] or None (proposals without a distribution),
     tokens int32 [batch][B], uniforms fp32 [batch][B + 1], drafted tokens int32
     [batch] -> (accepted, next_token, n_new), int32 [batch] each."""
+    if target_probs.dim() != 3:
+        raise LdrError(LDR_EINVAL, f"target_probs of {tuple(target_probs.shape)}")
     batch, B1, V = target_probs.shape
     B, dev = B1 - 1, target_probs.device
     _take(target_probs, (batch, B1, V), torch.float32, dev, "target_probs")
@@ -801,6 +809,8 @@ def verify_probs(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor]
         with _on(stream):
             workspace = torch.empty(verify_probs_workspace_bytes(batch, B, V), dtype=torch.uint8,
                                     device=dev)
+    _take(workspace, (workspace.numel(),), torch.uint8, dev, "workspace")
+    _on_gpu(dev, "verify_probs")
     acc, tok, n_new = out
     _check(_lib().ldr_verify_probs(_ptr(target_probs), _ptr(draft_probs), _ptr(draft_tokens),
                                    _ptr(n_draft), _ptr(uniforms), batch, B, V, _ptr(acc),

@@ -232,3 +232,13 @@ def test_binding_refuses_what_it_would_misread(L):
             L.verify_probs(*args)
     with pytest.raises(L.LdrError):
         L.verify_probs(P, None, y, u, n_draft=torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(L.LdrError, match="target_probs"):
+        L.verify_probs(P[0], None, y, u)
+    for ws in (torch.zeros(1 << 12), torch.zeros(2, 1 << 12, dtype=torch.uint8)):
+        with pytest.raises(L.LdrError, match="workspace"):
+            L.verify_probs(P, None, y, u, workspace=ws)
+    # host memory, otherwise as it should be
+    with pytest.raises(L.LdrError, match="verify_probs on cpu"):
+        L.verify_probs(P, None, y, u)
+    with pytest.raises(L.LdrError, match="Pages.init on cpu"):
+        p.init()
