@@ -349,9 +349,9 @@ int ldr_pages_fork(ldr_pages* p, const int32_t* src, void* stream);
 int ldr_pages_compact(ldr_pages* p, void* stream);
 
 /* Waits for `stream` and returns the sticky device status: LDR_OK, LDR_ERANGE,
- * LDR_EPAGES, or LDR_EINVAL once an ldr_attend ran on a plan that was not of the
- * cache's present state (the first of them that is set). Clears it if `clear` is
- * nonzero. */
+ * LDR_EPAGES, or LDR_EINVAL once an ldr_attend ran on a plan that was not this
+ * handle's of the cache's present state, and wrote nothing (the first of them that
+ * is set). Clears it if `clear` is nonzero. */
 int ldr_pages_status(ldr_pages* p, int clear, void* stream);
 
 /* Frees the handle; pool and state stay the caller's. NULL is ignored. */

@@ -3,6 +3,7 @@
 // kernels are in pages.hip and attend.hip.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -91,7 +92,8 @@ int ldr_pages_init(ldr_pages** out, const ldr_pages_config* cfg, void* pool, voi
   ldr_pages* p = new (std::nothrow) ldr_pages;
   if (!p) return LDR_ENOMEM;
   p->s = s;
-  p->p = PagesPtrs{static_cast<uint8_t*>(pool), static_cast<int32_t*>(state)};
+  static std::atomic<int32_t> handles{0};
+  p->p = PagesPtrs{static_cast<uint8_t*>(pool), static_cast<int32_t*>(state), ++handles};
   if (launch_pages_reset(s, p->p, static_cast<hipStream_t>(stream)) != hipSuccess) {
     delete p;
     return LDR_EHIP;

@@ -79,7 +79,7 @@ __device__ inline int tile_keys(int rows, int open, int share, int t, int rep, i
   return max(0, rows - open + t / rep + 1 - share) / unit * unit;
 }
 
-struct Header { int version, hq, max_new, items, pad[60]; };
+struct Header { int version, hq, max_new, items, id, pad[59]; };
 
 struct AttendWs {          // byte offsets in the workspace
   size_t map, info, items, ml, o, bytes;
@@ -341,6 +341,7 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
     hd->hq = hq;
     hd->max_new = max_new;
     hd->items = (int)n_items;
+    hd->id = p.id;
   }
   for (int c = wave; c < s.batch; c += NW)
     for (int i = lane; i < opens[c]; i += 64) map[qoffs[c] + i] = c * max_new + i;
@@ -455,11 +456,14 @@ __device__ inline SeqInfo scalar_info(const void* infos, size_t i) {
   return f;
 }
 
-// Whether the workspace holds a plan of the cache's present state for these
-// sizes; a workgroup that finds none records it and leaves.
+// Whether the workspace holds this handle's plan of the cache's present state for
+// these sizes; a workgroup that finds none records it and leaves, before it follows a
+// word of the plan. The handle's number stands for the layout of the workspace and of
+// the cache: another cache may have counted as many changes.
 __device__ inline bool plan_ok(const AttendArgs& a, int items) {
   const bool ok = scalar_word(a.ws, 0) == scalar_word(a.p.state, kPagesVersion) &&
                   scalar_word(a.ws, 1) == a.hq && scalar_word(a.ws, 2) == a.max_new &&
+                  scalar_word(a.ws, 4) == a.p.id &&
                   items >= 0 && items <= a.w.max_items;
   if (!ok && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.p.state + kPagesFlags, kFlagPlan);
   return ok;

@@ -187,13 +187,14 @@ struct PagesShape {
 };
 // Header words of the state.
 constexpr int kPagesFlags = 0;    // sticky flags
-constexpr int kPagesVersion = 1;  // counts the calls that change the tables
+constexpr int kPagesVersion = 1;  // counts the calls that change the tables, resets too
 constexpr int kPagesPairs = 2;    // pairs in the scratch list (compaction)
 constexpr int kPagesHeader = 64;
 constexpr int kFlagPages = 4;     // no room in the pool or a table
-constexpr int kFlagPlan = 8;      // an attention ran on a plan of another state
+constexpr int kFlagPlan = 8;      // an attention ran on a plan of another state or handle
 constexpr int kMaxSeqs = 1024;    // sequences of a cache: one thread each in the bookkeeping
-struct PagesPtrs { uint8_t* pool; int32_t* state; };
+// id: the handle's number, no other handle's of the process
+struct PagesPtrs { uint8_t* pool; int32_t* state; int32_t id; };
 hipError_t launch_pages_reset(const PagesShape& s, const PagesPtrs& p, hipStream_t st);
 hipError_t launch_pages_reserve(const PagesShape& s, const PagesPtrs& p, const int32_t* n_new,
                                 int max_new, hipStream_t st);

@@ -52,9 +52,13 @@ template <typename T> __device__ inline T block_scan(T v, T* sums, T* total) {
   return before + inc - v;
 }
 
+// The counter of changes goes on from what the memory holds: a plan of the cache that
+// was there before is no plan of the empty one.
 __global__ void __launch_bounds__(kBook) pages_reset_kernel(PagesShape s, PagesPtrs p) {
   const size_t i = blockIdx.x * (size_t)kBook + threadIdx.x;
-  if (i < s.words) p.state[i] = i >= s.table && i < s.refs ? -1 : 0;
+  if (i >= s.words) return;
+  if (i == kPagesVersion) p.state[i] = (int32_t)((uint32_t)p.state[i] + 1u);
+  else p.state[i] = i >= s.table && i < s.refs ? -1 : 0;
 }
 
 __global__ void pages_clear_flags_kernel(PagesPtrs p) { p.state[kPagesFlags] = 0; }
