@@ -786,6 +786,11 @@ attend_rows_kernel(AttendArgs a) {
         }
       }
     }
+    // a row without weight is 0, whatever values 0 was multiplied with
+#pragma unroll
+    for (int u = 0; u < NI; ++u)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[u][k] = ll[u] == 0.f ? 0.f : acc[u][k];
   }
 #pragma unroll
   for (int u = 0; u < NI; ++u) {
