@@ -386,12 +386,14 @@ int ldr_attend_plan(const ldr_pages* p, int32_t n_q_heads, int32_t max_new,
  * query head h over K/V head h / (n_q_heads / n_kv_heads). Products in the
  * cache's dtype, the probabilities rounded to it before they meet v; scores, sums
  * and the joining of partial results are fp32. A row that no key's score reaches
- * (all of them -inf) gives o = 0 and lse = -inf. What masked places hold does
- * not count, infinities and NaN included. Rows i >= open[b] of o and lse stay as
- * they were. n_q_heads and max_new are the plan's.
+ * (all of them -inf) gives o = 0 and lse = -inf; of other rows a key whose score is
+ * -inf still multiplies its v by 0. What masked places hold does not count,
+ * infinities and NaN included. Rows i >= open[b] of o and lse stay as they were.
+ * n_q_heads and max_new are the plan's.
  *   q    dev dtype, row (b, i) at q + (b max_new + i) q_stride elements, its
  *        [n_q_heads][head_dim] contiguous; q_stride a multiple of 8 (bf16) or 4
- *   o    dev [batch][max_new][n_q_heads][head_dim] dtype
+ *   o    dev [batch][max_new][n_q_heads][head_dim] dtype; may be q, if q is laid
+ *        out so
  *   lse  dev fp32 [batch][max_new][n_q_heads], or NULL
  *   scale  a normal number above 0 (1 / sqrt(head_dim) as a rule) */
 int ldr_attend(const ldr_pages* p, int32_t layer, const void* q, int64_t q_stride,

@@ -775,16 +775,32 @@ attend_rows_kernel(AttendArgs a) {
         const int i = u * kThreads + threadIdx.x, row = row_of(i), e = el_of(i);
         const int last = row < it.nr ? cbase + (it.r0 + row) / a.rep : -1;
         for (int k = it.k0 + s0 * kStep; k <= last; ++k) {
-          const T* vt = reinterpret_cast<const T*>(
-                            vpool + (size_t)clamp_page(a.s, table[k >> shift]) * a.s.page_bytes) +
-                        hoff + (k & (a.s.page - 1));
+          const size_t off = (size_t)clamp_page(a.s, table[k >> shift]) * a.s.page_bytes;
+          const int in = k & (a.s.page - 1);
+          const T* vt = reinterpret_cast<const T*>(vpool + off) + hoff + in;
+          float v[4];
+          bool any = false;
 #pragma unroll
           for (int d = 0; d < 4; ++d) {
-            const float v = Elem<T>::load(vt + (size_t)(e + d) * a.s.page);
-            if (!(fabsf(v) < INFINITY)) acc[u][d] += v;
+            v[d] = Elem<T>::load(vt + (size_t)(e + d) * a.s.page);
+            any = any || !(fabsf(v[d]) < INFINITY);
           }
+          if (!any) continue;
+          // a key without weight gives 0 x inf, as in the main kernel
+          const int rr = it.r0 + row, i = rr / a.rep;
+          const T* qr = static_cast<const T*>(a.q) +
+                        ((size_t)it.seq * a.max_new + i) * a.q_stride + (head * a.rep + rr - i * a.rep) * D;
+          const T* kr = reinterpret_cast<const T*>(kpool + off) + hoff + (size_t)in * D;
+          float sc = 0.f;
+#pragma unroll 1
+          for (int j = 0; j < D; ++j) sc += Elem<T>::load(qr + j) * Elem<T>::load(kr + j);
+          const float w = sc * c2 == -INFINITY ? 0.f : 1.f;
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+            if (!(fabsf(v[d]) < INFINITY)) acc[u][d] += w * v[d];
         }
       }
+      __syncthreads();      // q has been read: it may be o
     }
     // a row without weight is 0, whatever values 0 was multiplied with
 #pragma unroll
