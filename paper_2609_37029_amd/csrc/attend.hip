@@ -478,6 +478,15 @@ __device__ inline float other_half(float x) {
 __device__ inline float half_max(float x) { return fmaxf(x, other_half(x)); }
 __device__ inline float half_sum(float x) { return x + other_half(x); }
 
+// What scales the results so far from their maximum m to another, mu = max c2. The
+// product is rounded as mu was: fused with the difference it would leave mu's rounding
+// error where the maximum stays, and every step would scale by it (fp32, 512 rows, each
+// over 16384 keys of the score 7055: their mean off by 3.6e-3 instead of 1.7e-6).
+__device__ inline float rescale(float m, float c2, float mu) {
+#pragma clang fp contract(off)
+  return __builtin_amdgcn_exp2f(m * c2 - mu);
+}
+
 // The value of the column 16, 8, 4, 2 or 1 to the side, of the same half. By turns
 // for 8 and 4: of columns that agree at twice the distance, that is the same.
 template <int OFF> __device__ inline float aside(float x) {
@@ -690,7 +699,7 @@ attend_rows_kernel(AttendArgs a) {
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
     mx = half_max(mx);
     const float mn = fmaxf(m, mx), mu = mn == -INFINITY ? 0.f : mn * c2;
-    const float alpha = __builtin_amdgcn_exp2f(m * c2 - mu);
+    const float alpha = rescale(m, c2, mu);
     m = mn;
     float sum = 0.f;
 #pragma unroll
