@@ -176,10 +176,19 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
-def _stream(stream=None):
+def _stream(stream=None, device=None):
+    """The stream of a call: the given one, or the current one. With `device`, that of the
+    call's memory: refused unless it is current (and the stream's), as the kernels would run
+    on another GPU."""
+    if stream is not None and device is None:
+        return ctypes.c_void_p(stream.cuda_stream)
+    here = torch.cuda.current_device()
+    if device is not None and (device.index != here or
+                               (stream is not None and stream.device_index != here)):
+        raise LdrError(LDR_EINVAL, f"memory on {device}, current device {here}, stream {stream}")
     # torch.cuda.current_stream() makes a Stream object: 3 us, as long as a launch
     if stream is None:
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(here))
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -269,7 +278,8 @@ class Views:
         """ldr_views_fork: sequence b takes the views of sequence src[b] (int32
         [batch]); src[b] = b leaves it as it is, -1 resets it."""
         _take(src, (self.batch,), torch.int32, self.arena.device, "src")
-        _check(_lib().ldr_views_fork(self._h, _ptr(src), _stream(self._stream)), "ldr_views_fork")
+        _check(_lib().ldr_views_fork(self._h, _ptr(src), _stream(self._stream, self.arena.device)),
+               "ldr_views_fork")
 
     def status(self, clear: bool = False) -> int:
         return _lib().ldr_views_status(self._h, int(clear), _stream(self._stream))
@@ -650,13 +660,16 @@ class Pages:
         _on_gpu(self.device, "Pages.init")
         self.close()
         _check(_lib().ldr_pages_init(ctypes.byref(self._h), ctypes.byref(self.cfg),
-                                     _ptr(self.pool), _ptr(self.state), _stream(self._stream)),
+                                     _ptr(self.pool), _ptr(self.state), self._at()),
                "ldr_pages_init")
         return self
 
     @property
     def handle(self):
         return self._h
+
+    def _at(self):
+        return _stream(self._stream, self.device)
 
     def k(self, layer: int) -> torch.Tensor:
         """A layer's K pages [n_pages][n_kv_heads][page][head_dim]."""
@@ -671,7 +684,7 @@ class Pages:
         max_new), the sequence's open rows from here on."""
         _take(n_new, (self.batch,), torch.int32, self.device, "n_new")
         _check(_lib().ldr_pages_reserve(self._h, _ptr(n_new), int(max_new),
-                                        _stream(self._stream)), "ldr_pages_reserve")
+                                        self._at()), "ldr_pages_reserve")
 
     def write(self, K: torch.Tensor, V: torch.Tensor, layer: int = 0):
         """ldr_pages_write: the open rows from K and V [batch][max_new][layers]
@@ -680,7 +693,7 @@ class Pages:
         _take(K, shape, self.dtype, self.device, "K")
         _take(V, shape, self.dtype, self.device, "V")
         _check(_lib().ldr_pages_write(self._h, int(layer), shape[2], _ptr(K), _ptr(V), shape[1],
-                                      _stream(self._stream)), "ldr_pages_write")
+                                      self._at()), "ldr_pages_write")
 
     def append(self, n_new: torch.Tensor, K: torch.Tensor, V: torch.Tensor):
         """Reserve and write the rows of all layers, as Views.update takes them."""
@@ -692,20 +705,20 @@ class Pages:
     def keep(self, kept: torch.Tensor):
         """ldr_pages_keep: of the open rows, the first kept[b] (int32 [batch])."""
         _take(kept, (self.batch,), torch.int32, self.device, "kept")
-        _check(_lib().ldr_pages_keep(self._h, _ptr(kept), _stream(self._stream)), "ldr_pages_keep")
+        _check(_lib().ldr_pages_keep(self._h, _ptr(kept), self._at()), "ldr_pages_keep")
 
     def fork(self, src: torch.Tensor):
         """ldr_pages_fork: sequence b takes the pages of sequence src[b] (int32
         [batch]); src[b] = b leaves it as it is, -1 leaves it empty."""
         _take(src, (self.batch,), torch.int32, self.device, "src")
-        _check(_lib().ldr_pages_fork(self._h, _ptr(src), _stream(self._stream)), "ldr_pages_fork")
+        _check(_lib().ldr_pages_fork(self._h, _ptr(src), self._at()), "ldr_pages_fork")
 
     def compact(self):
         """ldr_pages_compact: the live pages to the lowest ids."""
-        _check(_lib().ldr_pages_compact(self._h, _stream(self._stream)), "ldr_pages_compact")
+        _check(_lib().ldr_pages_compact(self._h, self._at()), "ldr_pages_compact")
 
     def status(self, clear: bool = False) -> int:
-        return _lib().ldr_pages_status(self._h, int(clear), _stream(self._stream))
+        return _lib().ldr_pages_status(self._h, int(clear), self._at())
 
     def attend_workspace_bytes(self, n_q_heads: int, max_new: int) -> int:
         return int(_lib().ldr_attend_workspace_bytes(ctypes.byref(self.cfg), n_q_heads, max_new))
@@ -747,7 +760,7 @@ class AttendPlan:
         self.workspace = workspace
         _check(_lib().ldr_attend_plan(pages.handle, n_q_heads, max_new, _ptr(groups),
                                       _ptr(workspace), workspace.numel(),
-                                      _stream(pages._stream)), "ldr_attend_plan")
+                                      pages._at()), "ldr_attend_plan")
 
 
 def attend(plan: AttendPlan, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -773,7 +786,7 @@ def attend(plan: AttendPlan, layer: int, q: torch.Tensor, out: Optional[torch.Te
     scale = p.d ** -0.5 if scale is None else float(scale)
     _check(_lib().ldr_attend(p.handle, int(layer), _ptr(q), row, plan.n_q_heads,
                              plan.max_new, scale, _ptr(out), _ptr(lse), _ptr(plan.workspace),
-                             plan.workspace.numel(), _stream(p._stream)), "ldr_attend")
+                             plan.workspace.numel(), p._at()), "ldr_attend")
     return out
 
 
@@ -815,5 +828,5 @@ def verify_probs(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor]
     _check(_lib().ldr_verify_probs(_ptr(target_probs), _ptr(draft_probs), _ptr(draft_tokens),
                                    _ptr(n_draft), _ptr(uniforms), batch, B, V, _ptr(acc),
                                    _ptr(tok), _ptr(n_new), _ptr(workspace), workspace.numel(),
-                                   _stream(stream)), "ldr_verify_probs")
+                                   _stream(stream, dev)), "ldr_verify_probs")
     return out
