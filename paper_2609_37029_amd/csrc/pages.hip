@@ -55,10 +55,11 @@ template <typename T> __device__ inline T block_scan(T v, T* sums, T* total) {
 // The counter of changes goes on from what the memory holds: a plan of the cache that
 // was there before is no plan of the empty one.
 __global__ void __launch_bounds__(kBook) pages_reset_kernel(PagesShape s, PagesPtrs p) {
-  const size_t i = blockIdx.x * (size_t)kBook + threadIdx.x;
-  if (i >= s.words) return;
-  if (i == kPagesVersion) p.state[i] = (int32_t)((uint32_t)p.state[i] + 1u);
-  else p.state[i] = i >= s.table && i < s.refs ? -1 : 0;
+  for (size_t i = blockIdx.x * (size_t)kBook + threadIdx.x; i < s.words;
+       i += (size_t)gridDim.x * kBook) {
+    if (i == kPagesVersion) p.state[i] = (int32_t)((uint32_t)p.state[i] + 1u);
+    else p.state[i] = i >= s.table && i < s.refs ? -1 : 0;
+  }
 }
 
 __global__ void pages_clear_flags_kernel(PagesPtrs p) { p.state[kPagesFlags] = 0; }
@@ -371,8 +372,10 @@ int pieces_of(const PagesShape& s) { return (int)((s.page_bytes + kPiece - 1) / 
 }  // namespace
 
 hipError_t launch_pages_reset(const PagesShape& s, const PagesPtrs& p, hipStream_t st) {
-  hipLaunchKernelGGL(pages_reset_kernel, dim3((unsigned)((s.words + kBook - 1) / kBook)),
-                     dim3(kBook), 0, st, s, p);
+  // a launch holds fewer than 2^32 threads, the largest state 2^35 words
+  const size_t wgs = (s.words + kBook - 1) / kBook;
+  hipLaunchKernelGGL(pages_reset_kernel, dim3((unsigned)(wgs < 65536 ? wgs : 65536)), dim3(kBook), 0,
+                     st, s, p);
   return hipGetLastError();
 }
 
