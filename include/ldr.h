@@ -395,7 +395,8 @@ int ldr_attend_plan(const ldr_pages* p, int32_t n_q_heads, int32_t max_new,
  *   o    dev [batch][max_new][n_q_heads][head_dim] dtype; may be q, if q is laid
  *        out so
  *   lse  dev fp32 [batch][max_new][n_q_heads], or NULL
- *   scale  a normal number above 0 (1 / sqrt(head_dim) as a rule) */
+ *   scale  a normal number above 0 (1 / sqrt(head_dim) as a rule), at most 2^127; scores
+ *          beyond 2^127 may count as infinite */
 int ldr_attend(const ldr_pages* p, int32_t layer, const void* q, int64_t q_stride,
                int32_t n_q_heads, int32_t max_new, float scale, void* o, float* lse,
                void* workspace, size_t workspace_bytes, void* stream);

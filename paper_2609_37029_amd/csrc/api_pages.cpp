@@ -177,6 +177,7 @@ int ldr_attend(const ldr_pages* p, int32_t layer, const void* q, int64_t q_strid
   if (q_stride < (int64_t)n_q_heads * p->s.d || q_stride % (16 / (int64_t)p->s.el))
     return LDR_EINVAL;
   if (!std::isnormal(scale) || scale < 0.f) return LDR_EINVAL;
+  if (!std::isfinite(scale * kLog2e)) return LDR_EINVAL;   // the kernels' exponents are of base 2
   if (!workspace || !aligned(workspace, kAlign) ||
       workspace_bytes < attend_workspace_bytes(p->s, n_q_heads, max_new))
     return LDR_EINVAL;

@@ -587,7 +587,7 @@ attend_rows_kernel(AttendArgs a) {
   // the key of a step whose K row this lane loads
   const int mi = ((col >> 3) << 2) | (col & 3), mh = (col >> 2) & 1;
   const int krow = mi / E * 2 * E + mh * E + mi % E;
-  const float c2 = a.scale * 1.44269504088896341f;
+  const float c2 = a.scale * kLog2e;
   f32x16 o[ND] = {};
   float m = -INFINITY, l = 0.f;
   bool bad = false;   // V held a value that is not finite where a mask is
@@ -988,7 +988,7 @@ attend_wide_kernel(AttendArgs a) {
   const uint32_t klane = krow * (2 * D) + ((half ^ turn<KC>(krow)) << 4);
   const uint32_t vlane = col * 128 + ((half ^ turn<VC>(col)) << 4);
 
-  const float c2 = a.scale * 1.44269504088896341f;
+  const float c2 = a.scale * kLog2e;
   f32x16 o[ND] = {};
   float mu = -INFINITY, l = 0.f;
   f32x16 sc[2];

@@ -207,7 +207,8 @@ hipError_t launch_pages_fork(const PagesShape& s, const PagesPtrs& p, const int3
 hipError_t launch_pages_compact(const PagesShape& s, const PagesPtrs& p, hipStream_t st);
 hipError_t launch_pages_clear_flags(const PagesPtrs& p, hipStream_t st);
 
-// Attention over the paged cache (attend.hip).
+// Attention over the paged cache (attend.hip); exponents are of base 2.
+constexpr float kLog2e = 1.44269504088896341f;
 size_t attend_workspace_bytes(const PagesShape& s, int hq, int max_new);
 hipError_t launch_attend_plan(const PagesShape& s, const PagesPtrs& p, int hq, int max_new,
                               const int32_t* groups, void* ws, hipStream_t st);

@@ -95,3 +95,23 @@ def test_plan_of_a_state_put_back(gpu_lib):
     gpu_lib.attend(a.g.plan(4, 3), 0, q, out=out)
     assert a.g.status() == gpu_lib.LDR_OK
     check_attend(a, 3, q, out, None, 0, 0.125)
+
+
+def test_scales(gpu_lib):
+    """A scale whose product with log2(e) is no fp32 number is refused; the largest ones
+    that are not give what the definition does."""
+    a = _cache(gpu_lib, 2, F32)
+    q = a.rand(2, 3, 4, 64)
+    out = torch.full_like(q, 3.0)
+    for scale in (3e38, 2.0 ** 127 * 1.5):
+        with pytest.raises(gpu_lib.LdrError) as e:
+            gpu_lib.attend(a.g.plan(4, 3), 0, q, out=out, scale=scale)
+        assert e.value.code == gpu_lib.LDR_EINVAL and torch.all(out == 3.0)
+    q *= 2.0 ** -120
+    out = torch.zeros_like(q)
+    gpu_lib.attend(a.g.plan(4, 3), 0, q, out=out, scale=2.0 ** 117)
+    torch.cuda.synchronize()
+    check_attend(a, 3, q, out, None, 0, 2.0 ** 117)
+    gpu_lib.attend(a.g.plan(4, 3), 0, q * 0, out=out, scale=2.0 ** 127)
+    torch.cuda.synchronize()
+    check_attend(a, 3, q * 0, out, None, 0, 2.0 ** 127)
