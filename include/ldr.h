@@ -624,7 +624,8 @@ size_t ldr_verify_probs_workspace_bytes(int32_t batch, int32_t block, int32_t vo
  *   workspace    dev, ldr_verify_probs_workspace_bytes(batch, block, vocab)
  *                bytes, 16-byte aligned
  * LDR_EINVAL on a NULL pointer, a non-positive size, a batch above 65535, a block
- * or vocab above 2^30 or a short or misaligned workspace. */
+ * or vocab above 2^30, a short or misaligned workspace, or an output or workspace
+ * that overlaps an input or another of them. */
 int ldr_verify_probs(const float* target_probs, const float* draft_probs,
                      const int32_t* draft_tokens, const int32_t* n_draft, const float* uniforms,
                      int32_t batch, int32_t block, int32_t vocab, int32_t* accepted,

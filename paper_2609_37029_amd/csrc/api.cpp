@@ -123,6 +123,12 @@ static WsPlan plan_ws(const Shape& s, int batch) {
 
 static bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
+struct Range { const void* p; size_t bytes; };   // p null: none
+static bool overlap(const Range& a, const Range& b) {
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+}
+
 }  // namespace ldr
 
 using namespace ldr;
@@ -671,6 +677,19 @@ int ldr_verify_probs(const float* target_probs, const float* draft_probs,
     return LDR_EINVAL;
   const size_t need = ldr_verify_probs_workspace_bytes(batch, block, vocab);
   if (!need || workspace_bytes < need || !aligned(workspace, 16)) return LDR_EINVAL;
+  // every workgroup of a sequence reads the inputs while one writes its counts, and the
+  // second launch reads the first one's
+  const size_t rows = (size_t)batch * block, all = rows + batch;
+  const Range out[] = {{accepted, batch * 4ul}, {next_token, batch * 4ul}, {n_new, batch * 4ul},
+                       {workspace, need}};
+  const Range in[] = {{target_probs, all * vocab * 4}, {draft_probs, rows * vocab * 4},
+                      {draft_tokens, rows * 4}, {n_draft, batch * 4ul}, {uniforms, all * 4}};
+  for (const Range& o : out) {
+    for (const Range& i : in)
+      if (overlap(o, i)) return LDR_EINVAL;
+    for (const Range& x : out)
+      if (&x != &o && overlap(o, x)) return LDR_EINVAL;
+  }
   return launch_verify_probs(target_probs, draft_probs, draft_tokens, n_draft, uniforms, batch,
                              block, vocab, accepted, next_token, n_new, workspace,
                              static_cast<hipStream_t>(stream)) == hipSuccess
