@@ -13,11 +13,11 @@
 // mask runs (or all of a sequence's own where they are few), go to the last kernel,
 // which also joins the parts of its rows.
 //
-// Measured with 32 query and 8 K/V heads of 128, bf16, a layer: 64 sequences with one row,
-// 32768 keys in common and 300 of their own 47 us + 27 us in the last kernel (the shared
-// keys alone are 28 us of a large matrix product); 16 with 17 rows and 512 keys of their
-// own 185 + 29 (116); 16 with 17 rows and up to 8192 keys of their own, none in common,
-// 95 + 17 (4.7 TB/s); 2 with 512 rows over 8192 keys 146 + 33.
+// Measured with 32 query and 8 K/V heads of 128, bf16, a layer, passes in a loop: 64
+// sequences with one row, 32768 keys in common and 300 of their own 48 us + 27 us in the
+// last kernel (the shared keys alone are 28 us of a large matrix product); 16 with 17 rows
+// and 512 keys of their own 152 + 25 (115); 16 with 17 rows and up to 8192 keys of their
+// own, none in common, 94 + 15 (4.8 TB/s); 2 with 512 rows over 8192 keys 129 + 28 (109).
 #include <type_traits>
 
 #include "ldr_internal.h"
@@ -40,20 +40,24 @@ constexpr int kStage = 64;           // keys of a stage of the bf16 main kernel
 constexpr int kMinShared = 256;
 // Keys of a sequence's own that are worth items; fewer are left to the last kernel. 64
 // sequences as above with 32768 keys in common: 167 us, 181 if their 256 keys become
-// items; with 700 keys of their own 139 us, 154 if they do not.
+// items; with 700 keys of their own 139 us, 154 if they do not. Fresh prompts, all rows
+// open, a layer: one of 300 14.7 us, 20.2 if its 256 keys become items; one of 512 20.2 and
+// 26.0, eight of 300 55 and 59, but four of 512 61 and 54.
 constexpr int kMinMain = 512;
 constexpr int kBlock = 32;           // rows of a block of partial results
 
 // Tiles of a dtype's main kernel: rows of an item, the keys that an item's are a
 // multiple of (four stages: the bf16 kernel's loop has no branch), workgroups that
-// run at once, and the keys whose work an item costs on top of its own (its start,
-// and writing and joining its part).
+// the plan cuts the work for, and the keys whose work an item costs on top of its own
+// (its start, and writing and joining its part). 256 bf16 workgroups run at once (by their
+// LDS with head_dim 128, by the registers that the kernel asks for with 64); 768 of fp32 run
+// with head_dim 64 and 256 with 128, and are cut for as 512.
 struct Tile { int rows, unit, slots, cost; };
 __host__ __device__ constexpr Tile tile_of(bool bf16) {
   return bf16 ? Tile{256, 4 * kStage, 256, 384} : Tile{32, 128, 512, 192};
 }
 __host__ __device__ inline Tile tile_of(const PagesShape& s) { return tile_of(s.dtype == LDR_BF16); }
-// Rounds of items over the workgroups that run at once, at most (4 took 2% longer: the
+// Rounds of items over those workgroups, at most (4 took 2% longer: the
 // grid is sized for as many, and most of it ends at once).
 constexpr int kMaxRounds = 2;
 
@@ -155,7 +159,7 @@ __device__ inline int even_step(int len, int n, int unit) {
 }
 
 // The plan, in one workgroup: thread b has sequence b; what looks at all
-// sequences for each goes by waves, a sequence at a time. 7.5 us for one sequence, 21 for
+// sequences for each goes by waves, a sequence at a time. 5.7 us for one sequence, 23 for
 // 64 with 512 pages in common (their tables, 128 KB, through one compute unit): once
 // for all layers.
 template <bool BF16>
@@ -379,6 +383,13 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
 // of row (or column) lane % 32, the E that half lane / 32 holds of 2 E
 // consecutive ones. The accumulator of lane l holds column l % 32; entry i is row
 // 8 (i / 4) + 4 (l / 32) + i % 4.
+//
+// Probabilities of a bf16 cache are rounded to bf16 where they meet V, half a step (2^-8) of
+// each at most; their sum takes them unrounded, so that lse is not touched. With a second
+// product for what the rounding leaves, o differs from its definition by 0.0017 (root mean
+// square, relative: its own rounding to bf16) instead of 0.0023, but it is half as much matrix
+// work again: five layers of the sequences above take 436 instead of 393 us, 1110 instead of
+// 893, 572 instead of 553 and 989 instead of 787. fp32 caches keep fp32.
 template <typename T> struct Mma;
 template <> struct Mma<uint16_t> {
   static constexpr int E = 8;
@@ -539,7 +550,7 @@ __device__ inline float2* part_ml(const AttendArgs& a, int head, long block) {
 // FINISH: the rows' parts, which the waves take in turn, and their last keys, where the
 // mask runs; then the results are written. Bound by bytes where parts and keys are many (64
 // sequences with one row: 34 MB of parts and 78 MB of keys in 27 us), else by the chain
-// of loads (plan, table, keys, V; 9 us for one sequence). Else: an item of the f32 main
+// of loads (plan, table, keys, V; 8 us for one sequence). Else: an item of the f32 main
 // kernel, its results a part (7 us for 2048 keys of 4 heads of 64).
 template <typename T, int D, bool FINISH>
 __global__ void __launch_bounds__(kThreads, sizeof(T) * D <= 256 ? 2 : 1)
@@ -869,7 +880,6 @@ template <int C> __device__ inline int turn(int r) {
   static_assert(C == 16 || C == 8, "rows of 256 or 128 bytes");
   return C == 16 ? r & 15 : (r >> 1) & 7;
 }
-#define LDR_GP(p) ((__attribute__((address_space(1))) void*)(p))
 #define LDR_LP(p) ((__attribute__((address_space(3))) void*)(p))
 
 // SMALL: pages of 32 rows, half a stage.

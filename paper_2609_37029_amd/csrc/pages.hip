@@ -6,10 +6,10 @@
 // first. References are counted with atomic adds, which commute. What moves
 // bytes (rows into pages, whole pages) runs over the GPU and is bound by HBM.
 //
-// Measured, Qwen3-8B heads, five layers, pages of 64: reserve 5 us, keep 2, fork 5 (64
-// sequences); rows of 64 x 17 tokens 16 us (45 MB in and out), of 16 x 17 7 us; copies of
-// 64 pages 26 us (84 MB written, the source in cache); compaction of half the pages of 32
-// x 4096 rows 256 us (1.2 GB, 4.7 TB/s).
+// Measured, Qwen3-8B heads, five layers, pages of 64: reserve 6 us, keep 2, fork 5 (64
+// sequences); rows of 64 x 17 tokens 16 us (45 MB in and out, 2.8 TB/s), of 16 x 17 7 us;
+// copies of 64 pages 26 us (84 MB written, 3.2 TB/s, the source in cache); compaction of half
+// the pages of 32 x 4096 rows 6 + 258 us (1.2 GB, 4.7 TB/s).
 #include "ldr_internal.h"
 
 namespace ldr {

@@ -12,7 +12,7 @@
 //
 // Bound by reading one target and one draft row a sequence, once, and at small
 // batches by the latency of the chain: tokens, gathers, rows, sums, second launch,
-// part. 64 sequences of 151936 tokens: sums 17 us (78 MB, 4.5 TB/s), draw 5 us; one: 5
+// part. 64 sequences of 151936 tokens: sums 18 us (78 MB, 4.3 TB/s), draw 4 us; one: 6
 // and 4. With a workgroup a part of 4096, and without the next part's loads under way,
 // 64 took 56 and 41 us.
 #include "ldr_internal.h"
@@ -279,7 +279,8 @@ hipError_t launch_verify_probs(const float* P, const float* Q, const int32_t* y,
   const int parts = (V + kPart - 1) / kPart;
   // A wave's parts: its workgroup tests the candidates first, and its next part's
   // loads need one before them; but 4096 waves, 4 a SIMD, come first. 64 sequences of
-  // 151936 tokens: 30.1 us with 2 parts a wave, 31.2 with 3, 32.9 with 4, 36 with 8.
+  // 151936 tokens, both launches: 24.4 us with 1 part a wave, 23.5 with 2, 24.9 with 3, 26.2
+  // with 4, 30.0 with 8.
   const int run = max(1, min(8, (int)((long)parts * batch / 4096)));
   ProbsArgs a{P, Q, y, n_draft, u, batch, B, V, parts, run, static_cast<Part*>(ws), accepted, token,
               n_new};
