@@ -48,7 +48,9 @@ enum ldr_status {
   LDR_EPAGES = -6   /* a sequence found no room in the page pool or its table */
 };
 
-enum ldr_dtype { LDR_F32 = 0, LDR_BF16 = 1 };
+/* The last two name what a paged cache holds its bf16 rows in, and nothing else
+ * (ldr_pages_config). */
+enum ldr_dtype { LDR_F32 = 0, LDR_BF16 = 1, LDR_MXFP4 = 4, LDR_MXFP8 = 8 };
 
 /* Views an ablation variant leaves out (Sec. 3.4, App. D.3): bits of
  * ldr_config.drop_views. A dropped view is neither kept nor read: its arena
@@ -278,6 +280,21 @@ void ldr_views_destroy(ldr_views* v);
  *          library. A copy of the whole state, put back later, undoes what
  *          calls in between did to the tables, not to the pool.
  *
+ * A cache of LDR_MXFP8 or LDR_MXFP4 takes and gives bf16 rows (K, V, q, o) and
+ * holds them as codes of 8 (e4m3) or 4 bits (e2m1), 32 consecutive dimensions
+ * of a row sharing a scale 2^e: 8.25 and 4.25 bits a value. e is the smallest
+ * exponent, -117 (-125) at least, with |x| <= 464 2^e (7 2^e) for all of the 32;
+ * a code is x / 2^e rounded to nearest, ties to even, at most 448 (6). So a value
+ * is off by half a step of its binade at most: 2^-4 (2^-2) of itself, or 2^(e-10)
+ * (2^(e-2)) where that is more. Magnitudes above 1.875 2^127 (1.5 2^127) count as
+ * that; a block with an infinity or a NaN is NaN as a whole. Codes stand for bf16
+ * numbers exactly; a row's codes do not depend on other rows. A head's rows of a page
+ * of that pool, in bytes:
+ *   K  [page][head_dim / 2] pairs of dimensions, then [page][head_dim / 32] scales
+ *   V  [head_dim / 2][page] pairs, then [head_dim / 32][page] scales
+ * a pair two bytes of 8-bit codes or one of 4-bit codes (the even dimension in
+ * the low bits), a scale the byte e + 127, or 255 for NaN.
+ *
  * Calls on one handle must be ordered (one stream, or streams joined by
  * events), and run with the device current that holds its memory. A table
  * entry or a length that is out of range (only a caller's own writes can leave
@@ -290,7 +307,8 @@ typedef struct ldr_pages_config {
   int32_t n_pages;       /* pages of the pool                                 */
   int32_t batch;         /* sequences, 1 .. 1024                              */
   int32_t max_pages;     /* pages of a sequence; max_pages * page < 2^30      */
-  int32_t dtype;         /* enum ldr_dtype of the pool                        */
+  int32_t dtype;         /* enum ldr_dtype: the rows' in and out and the pool's;
+                            LDR_MXFP8, LDR_MXFP4: bf16 rows, coded in the pool */
 } ldr_pages_config;
 
 typedef struct ldr_pages ldr_pages; /* opaque host handle */
@@ -324,9 +342,21 @@ int ldr_pages_reserve(ldr_pages* p, const int32_t* n_new, int32_t max_new, void*
  * row r of K and V (r < min(open[b], max_new)) is the sequence's row
  * rows[b] - open[b] + r. max_new is the reserve's, at most 2^28. With all
  * layers these are the K_new and V_new of ldr_views_update.
- *   K, V  dev [batch][max_new][n_layers][n_kv_heads][head_dim] dtype */
+ *   K, V  dev [batch][max_new][n_layers][n_kv_heads][head_dim] dtype (bf16 for
+ *         a coded cache) */
 int ldr_pages_write(ldr_pages* p, int32_t layer, int32_t n_layers, const void* K, const void* V,
                     int32_t max_new, void* stream);
+
+/* Reads rows back: row first[b] + r of sequence b, r < n[b], in layers [layer,
+ * layer + n_layers) to row r of K and V, as ldr_pages_write takes them (a coded
+ * cache's: the values that its codes stand for). Rows r >= n[b] of K and V stay as
+ * they were. A sequence whose range is not within its rows, or whose n[b] is
+ * outside [0, max_rows], is left out whole and sets the sticky LDR_ERANGE flag.
+ *   first, n  dev int32 [batch]
+ *   K, V      dev [batch][max_rows][n_layers][n_kv_heads][head_dim], of the rows'
+ *             type, 16-byte aligned */
+int ldr_pages_read(const ldr_pages* p, int32_t layer, int32_t n_layers, const int32_t* first,
+                   const int32_t* n, void* K, void* V, int32_t max_rows, void* stream);
 
 /* Keeps the first kept[b] open rows of every sequence and drops those behind
  * them, as a verification decides (its n_new); the kept ones stay open. Pages
@@ -390,7 +420,8 @@ int ldr_attend_plan(const ldr_pages* p, int32_t n_q_heads, int32_t max_new,
  * -inf still multiplies its v by 0. What masked places hold does not count,
  * infinities and NaN included. Rows i >= open[b] of o and lse stay as they were.
  * n_q_heads and max_new are the plan's.
- *   q    dev dtype, row (b, i) at q + (b max_new + i) q_stride elements, its
+ * A coded cache is attended to as a bf16 cache of the values that its codes stand for.
+ *   q    dev dtype (bf16 for a coded cache), row (b, i) at q + (b max_new + i) q_stride elements, its
  *        [n_q_heads][head_dim] contiguous; q_stride a multiple of 8 (bf16) or 4
  *   o    dev [batch][max_new][n_q_heads][head_dim] dtype; may be q, if q is laid
  *        out so
@@ -631,6 +662,40 @@ int ldr_verify_probs(const float* target_probs, const float* draft_probs,
                      int32_t batch, int32_t block, int32_t vocab, int32_t* accepted,
                      int32_t* next_token, int32_t* n_new, void* workspace,
                      size_t workspace_bytes, void* stream);
+
+/* Workspace bytes ldr_logprobs needs (0 on a size that it refuses). */
+size_t ldr_logprobs_workspace_bytes(int32_t batch, int32_t rows, int32_t vocab, int32_t top_n);
+
+/* Log probabilities of given tokens, as a server answers with them beside the tokens
+ * that a verification emitted or that a prompt consists of. With p = softmax(z / T) of
+ * row (b, i), i < n_rows[b], and y its token:
+ *   logp    log p(y); -inf for a y outside [0, vocab)
+ *   entropy - sum_v p(v) log p(v), in nats (0 log 0 = 0)
+ *   rank    entries before y's in the order by z, larger first, of equal ones the lower
+ *           index first (0: y is the row's argmax); vocab for a y outside [0, vocab)
+ *   top_tokens, top_logp  the first top_n tokens in that order and their log p
+ * An entry that is -inf has p = 0. A row of nothing else has log p = -inf
+ * everywhere and entropy 0; a NaN (which ranks behind every number) or a +inf in a row
+ * makes its log p and entropy NaN. Sums are fp32, in an order that depends on the sizes
+ * alone. Rows i >= n_rows[b] of the outputs stay as they were.
+ *   logits  dev fp32, row (b, i) at logits + (b rows + i) row_stride elements
+ *   tokens  dev int32 [batch][rows]
+ *   n_rows  dev int32 [batch] (a verification's n_new), or NULL: rows
+ *   temperature  T, a normal number above 0 whose log2(e) / T is one too (the greedy
+ *           sampler's 0 is refused: give the T that the probabilities are to be of)
+ *   top_n   0 .. 64, at most vocab; 0: top_tokens and top_logp may be NULL
+ *   logp, entropy  dev fp32 [batch][rows]; rank dev int32 [batch][rows]
+ *   top_tokens  dev int32 [batch][rows][top_n]; top_logp dev fp32 [batch][rows][top_n]
+ *   workspace   dev, ldr_logprobs_workspace_bytes(batch, rows, vocab, top_n) bytes,
+ *           256-byte aligned
+ * LDR_EINVAL on a NULL pointer, a size outside these (batch and rows at most 65535, vocab
+ * at most 2^30, row_stride from vocab to 2^40), a short or misaligned workspace, or an
+ * output or workspace that overlaps an input or another of them. */
+int ldr_logprobs(const float* logits, int64_t row_stride, const int32_t* tokens,
+                 const int32_t* n_rows, int32_t batch, int32_t rows, int32_t vocab,
+                 float temperature, int32_t top_n, float* logp, float* entropy, int32_t* rank,
+                 int32_t* top_tokens, float* top_logp, void* workspace, size_t workspace_bytes,
+                 void* stream);
 
 /* Writes Gumbel noise of the samplers' layout: out[r][e] = -log(-log(u)) of
  * entry e of row r in noise stream noise_stream (0: ldr_sample's token noise

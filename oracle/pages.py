@@ -1,6 +1,7 @@
 """Plain numpy forms of the operators around a drafting round: the paged cache
 (sequence by sequence, page by page), causal attention over it, verification
-from given probabilities, and forks of sequences. fp64 throughout."""
+from given probabilities, forks of sequences, rows held in 8 or 4 bits, and log
+probabilities of given tokens. fp64 throughout."""
 from __future__ import annotations
 
 import numpy as np
@@ -175,3 +176,74 @@ def verify_probs(P, Q, y, n, u):
     c = np.cumsum(w)
     over = np.flatnonzero((w > 0) & (c > u[B] * c[-1]))
     return r, int(over[0] if len(over) else some[-1])
+
+
+# Rows in codes: the magnitudes of a code, the limit of a block's largest one in units of
+# its scale, the lowest exponent, the largest magnitude that is coded as it is.
+def _e4m3(code):
+    e, m = code >> 3, code & 7
+    return m * 2.0 ** -9 if e == 0 else (8 + m) * 2.0 ** (e - 10)
+
+
+MX = {4: ([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], 7.0, -125, 1.5 * 2.0 ** 127),
+      8: ([_e4m3(c) for c in range(127)], 464.0, -117, 1.875 * 2.0 ** 127)}
+
+
+def mx_values(x, bits):
+    """What rows [..., d] are held as: 32 dimensions share the smallest scale 2^e that
+    their largest magnitude is within the limit of; each is the nearest code, the one of
+    even number where two are as near."""
+    grid, limit, lowest, top = MX[bits]
+    grid = np.array(grid)
+    x = np.asarray(x, np.float64)
+    blocks = x.reshape(-1, 32)
+    bad = ~np.isfinite(blocks).all(1, keepdims=True)
+    blocks = np.clip(np.where(bad, 0.0, blocks), -top, top)
+    scales = 2.0 ** np.arange(lowest, 128)
+    most = np.abs(blocks).max(1, keepdims=True)
+    scale = scales[np.searchsorted(limit * scales, most)]         # the first that holds it
+    y = np.abs(blocks) / scale
+    hi = np.minimum(np.searchsorted(grid, y), len(grid) - 1)      # the codes around
+    lo = np.maximum(hi - 1, 0)
+    up, down = np.abs(grid[hi] - y), np.abs(y - grid[lo])
+    code = np.where((up < down) | ((up == down) & (hi % 2 == 0)), hi, lo)
+    out = np.where(bad, np.nan, np.copysign(grid[code] * scale, blocks))
+    return out.reshape(x.shape)
+
+
+class CodedCache(Cache):
+    """A cache that holds its rows in 8 or 4 bits."""
+
+    def __init__(self, bits, *sizes):
+        super().__init__(*sizes)
+        self.bits = bits
+
+    def write(self, K, V, layer=0):
+        super().write(mx_values(K, self.bits), mx_values(V, self.bits), layer)
+
+
+def logprobs(z, y, temperature, top):
+    """One row of logits: (log p(y), entropy, rank of y, the first `top` tokens, their log p)."""
+    z = np.asarray(z, np.float64)
+    V = len(z)
+    ahead = lambda v: (np.isnan(z[v]), -z[v] if not np.isnan(z[v]) else 0.0, v)  # noqa: E731
+    order = sorted(range(V), key=ahead)[:top] if V <= 4096 else list(
+        np.lexsort((np.arange(V), -np.where(np.isnan(z), -np.inf, z), np.isnan(z)))[:top])
+    given = 0 <= y < V
+    rank = V
+    if given:
+        numbers = ~np.isnan(z)
+        first = np.arange(V) < y
+        rank = int((z > z[y]).sum() + ((z == z[y]) & first).sum()) if numbers[y] else \
+            int(numbers.sum() + (~numbers & first).sum())
+    if np.isnan(z).any() or np.isposinf(z).any():
+        return np.nan, np.nan, rank, order, np.full(top, np.nan)
+    if np.all(np.isneginf(z)):
+        return -np.inf, 0.0, rank, order, np.full(top, -np.inf)
+    x = (z - z.max()) / temperature
+    p = np.exp(x)
+    # the entries at the maximum are 1 each: their number is kept apart from the others' sum
+    ls = np.log1p((x == 0).sum() - 1 + p[x != 0].sum())
+    some = p > 0
+    entropy = ls - (p[some] * x[some]).sum() / p.sum()
+    return (x[y] - ls if given else -np.inf), entropy, rank, order, x[order] - ls

@@ -24,11 +24,15 @@ static bool make_pages_shape(const ldr_pages_config* c, PagesShape* s) {
   if (c->n_pages < 1 || c->n_pages > (1 << 28)) return false;
   if (c->batch < 1 || c->batch > kMaxSeqs) return false;
   if (c->max_pages < 1 || (int64_t)c->max_pages * c->page >= (1 << 30)) return false;
-  if (c->dtype != LDR_F32 && c->dtype != LDR_BF16) return false;
+  if (c->dtype != LDR_F32 && c->dtype != LDR_BF16 && c->dtype != LDR_MXFP4 &&
+      c->dtype != LDR_MXFP8)
+    return false;
   s->layers = c->n_layers; s->hkv = c->n_kv_heads; s->d = c->head_dim; s->page = c->page;
   s->n_pages = c->n_pages; s->batch = c->batch; s->max_pages = c->max_pages; s->dtype = c->dtype;
-  s->el = c->dtype == LDR_BF16 ? 2 : 4;
-  s->page_bytes = (size_t)s->hkv * s->page * s->d * s->el;
+  s->bits = c->dtype == LDR_MXFP4 ? 4 : c->dtype == LDR_MXFP8 ? 8 : 0;
+  s->el = c->dtype == LDR_F32 ? 4 : 2;
+  s->head_bytes = (size_t)s->page * (s->bits ? s->d * s->bits / 8 + s->d / kMxBlock : s->d * s->el);
+  s->page_bytes = s->hkv * s->head_bytes;
   // regions start on 256 bytes
   auto words = [](size_t n) { return align_up(n * 4) / 4; };
   size_t off = kPagesHeader;
@@ -115,6 +119,17 @@ int ldr_pages_write(ldr_pages* p, int32_t layer, int32_t n_layers, const void* K
     return LDR_EINVAL;
   return done(launch_pages_write(p->s, p->p, layer, n_layers, K, V, max_new,
                                  static_cast<hipStream_t>(stream)));
+}
+
+int ldr_pages_read(const ldr_pages* p, int32_t layer, int32_t n_layers, const int32_t* first,
+                   const int32_t* n, void* K, void* V, int32_t max_rows, void* stream) {
+  if (!p || layer < 0 || n_layers < 1 || layer >= p->s.layers || n_layers > p->s.layers - layer)
+    return LDR_EINVAL;
+  if (!first || !n || !aligned(first, 4) || !aligned(n, 4)) return LDR_EINVAL;
+  if (max_rows < 1 || max_rows > (1 << 28) || !K || !V || !aligned(K, 16) || !aligned(V, 16))
+    return LDR_EINVAL;
+  return done(launch_pages_read(p->s, p->p, layer, n_layers, first, n, K, V, max_rows,
+                                static_cast<hipStream_t>(stream)));
 }
 
 int ldr_pages_keep(ldr_pages* p, const int32_t* kept, void* stream) {

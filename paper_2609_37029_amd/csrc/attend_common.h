@@ -1,0 +1,356 @@
+// What the attention kernels over the paged cache share: the plan's items and
+// layout (attend.hip writes them), matrix products, and the joining of partial
+// results. Included by one source file a kind of cache, hence the unnamed namespace.
+#ifndef LDR_ATTEND_COMMON_H
+#define LDR_ATTEND_COMMON_H
+
+#include <type_traits>
+
+#include "ldr_internal.h"
+
+namespace ldr {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+constexpr int kWideThreads = 512;
+constexpr int kBook = 1024;          // threads of the plan's workgroup
+constexpr int kStep = 32;            // keys of a step; a page holds whole steps
+constexpr int kStage = 64;           // keys of a stage of the bf16 main kernel
+// Keys in common that are worth a segment of their own. 64 sequences with one row, 300
+// keys of their own and as many in common, two layers: 77 us with the segment and 88
+// without at 256 keys, 76 and 97 at 512.
+constexpr int kMinShared = 256;
+// Keys of a sequence's own that are worth items; fewer are left to the last kernel. 64
+// sequences as above with 32768 keys in common: 167 us, 181 if their 256 keys become
+// items; with 700 keys of their own 139 us, 154 if they do not. Fresh prompts, all rows
+// open, a layer: one of 300 14.7 us, 20.2 if its 256 keys become items; one of 512 20.2 and
+// 26.0, eight of 300 55 and 59, but four of 512 61 and 54.
+constexpr int kMinMain = 512;
+constexpr int kBlock = 32;           // rows of a block of partial results
+
+// Tiles of a dtype's main kernel: rows of an item, the keys that an item's are a
+// multiple of (four stages: the bf16 kernel's loop has no branch), workgroups that
+// the plan cuts the work for, and the keys whose work an item costs on top of its own
+// (its start, and writing and joining its part). 256 bf16 workgroups run at once (by their
+// LDS with head_dim 128, by the registers that the kernel asks for with 64); 768 of fp32 run
+// with head_dim 64 and 256 with 128, and are cut for as 512.
+struct Tile { int rows, unit, slots, cost; };
+__host__ __device__ constexpr Tile tile_of(bool bf16) {
+  return bf16 ? Tile{256, 4 * kStage, 256, 384} : Tile{32, 128, 512, 192};
+}
+__host__ __device__ inline Tile tile_of(const PagesShape& s) { return tile_of(s.dtype != LDR_F32); }
+// Rounds of items over those workgroups, at most (4 took 2% longer: the
+// grid is sized for as many, and most of it ends at once).
+constexpr int kMaxRounds = 2;
+
+__device__ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+// One unit of work: rows r0 .. r0 + nr of a segment over keys k0 .. k1 of
+// sequence seq. Row r belongs to the segment's query r / rep, entry q0 + r / rep
+// of the row map, head r % rep of the group. Partial results go to blocks of 32
+// rows from `part` on.
+struct Item { int q0, r0, nr, seq, k0, k1, part, pad; };
+
+// A sequence: its first entry in the row map, open rows, keys, and the keys it
+// leaves to its group; its own chunks of `step` keys (0: none), chunk c of its
+// row r in block own_part + c own_blocks + r / 32; the same for its group's chunks
+// and its row grp_off + r there.
+struct SeqInfo {
+  int qoff, open, rows, share, step, own_part, own_chunks, own_blocks;
+  int grp_part, grp_chunks, grp_blocks, grp_off, pad[4];
+};
+static_assert(sizeof(Item) == 32 && sizeof(SeqInfo) == 64, "read as words");
+
+// Keys, from `share` on, that every row of the tile from row t on sees and items
+// can take: whole units.
+__device__ inline int tile_keys(int rows, int open, int share, int t, int rep, int unit) {
+  return max(0, rows - open + t / rep + 1 - share) / unit * unit;
+}
+
+struct Header { int version, hq, max_new, items, id, pad[59]; };
+
+struct AttendWs {          // byte offsets in the workspace
+  size_t map, info, items, ml, o, bytes;
+  int max_items;
+  int tiles;               // of 32 rows of a sequence
+  long blocks;             // of partial results, per K/V head
+};
+
+// Items of one K/V head that the chunks add to a cut by tiles alone.
+__host__ __device__ inline int added_items(const PagesShape& s) {
+  return kMaxRounds * tile_of(s).slots / s.hkv + 1;
+}
+
+AttendWs plan_ws(const PagesShape& s, int hq, int max_new) {
+  AttendWs w;
+  const int rep = hq / s.hkv, tile = tile_of(s).rows;
+  const long rows = (long)s.batch * max_new * rep;
+  // every tile of the own and of the shared segments once, and the added ones
+  w.max_items = (int)((long)s.batch * (((long)max_new * rep + tile - 1) / tile) + rows / tile +
+                      s.batch / 2 + added_items(s));
+  w.tiles = (int)(((long)max_new * rep + kBlock - 1) / kBlock);
+  w.blocks = (long)s.batch * w.tiles + rows / kBlock + s.batch / 2 +
+             (long)(tile / kBlock) * added_items(s);
+  size_t off = sizeof(Header);
+  w.map = off; off = align_up(off + (size_t)s.batch * max_new * 4);
+  w.info = off; off = align_up(off + (size_t)s.batch * sizeof(SeqInfo));
+  w.items = off; off = align_up(off + (size_t)w.max_items * sizeof(Item));
+  w.ml = off; off = align_up(off + (size_t)s.hkv * w.blocks * kBlock * 8);
+  w.o = off; off = align_up(off + (size_t)s.hkv * w.blocks * kBlock * s.d * 4);
+  w.bytes = off;
+  return w;
+}
+
+__device__ inline int clamp_rows(const PagesShape& s, int r) {
+  return min(max(r, 0), s.max_pages * s.page);
+}
+__device__ inline int clamp_page(const PagesShape& s, int id) {
+  return min(max(id, 0), s.n_pages - 1);
+}
+
+// Matrix products of 32 x 32 tiles. A fragment is 16 bytes a lane: E elements
+// of row (or column) lane % 32, the E that half lane / 32 holds of 2 E
+// consecutive ones. The accumulator of lane l holds column l % 32; entry i is row
+// 8 (i / 4) + 4 (l / 32) + i % 4.
+//
+// Probabilities of a bf16 cache are rounded to bf16 where they meet V, half a step (2^-8) of
+// each at most; their sum takes them unrounded, so that lse is not touched. With a second
+// product for what the rounding leaves, o differs from its definition by 0.0017 (root mean
+// square, relative: its own rounding to bf16) instead of 0.0023, but it is half as much matrix
+// work again: five layers of the sequences above take 436 instead of 393 us, 1110 instead of
+// 893, 572 instead of 553 and 989 instead of 787. fp32 caches keep fp32.
+template <typename T> struct Mma;
+template <> struct Mma<uint16_t> {
+  static constexpr int E = 8;
+  __device__ static f32x16 run(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  __device__ static u32x4 pack(const float* x) {   // probabilities, rounded to bf16
+    bf16x8 v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (__bf16)x[j];
+    return __builtin_bit_cast(u32x4, v);
+  }
+  __device__ static void store4(uint16_t* o, const float* x) {
+    uint2 v{f32_to_bf16(x[0]) | (uint32_t)f32_to_bf16(x[1]) << 16,
+            f32_to_bf16(x[2]) | (uint32_t)f32_to_bf16(x[3]) << 16};
+    *reinterpret_cast<uint2*>(o) = v;
+  }
+  __device__ static float get(u32x4 v, int j) {
+    return __uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16);
+  }
+};
+template <> struct Mma<float> {
+  static constexpr int E = 4;
+  __device__ static f32x16 run(u32x4 a, u32x4 b, f32x16 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[j]), __uint_as_float(b[j]), c, 0,
+                                               0, 0);
+    return c;
+  }
+  __device__ static u32x4 pack(const float* x) {
+    return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
+                 __float_as_uint(x[3])};
+  }
+  __device__ static void store4(float* o, const float* x) {
+    *reinterpret_cast<float4*>(o) = float4{x[0], x[1], x[2], x[3]};
+  }
+  __device__ static float get(u32x4 v, int j) { return __uint_as_float(v[j]); }
+};
+
+struct AttendArgs {
+  PagesShape s;
+  PagesPtrs p;
+  const void* q; long q_stride;
+  void* o; float* lse;
+  int layer, hq, rep, max_new;
+  float scale;
+  uint8_t* ws;
+  AttendWs w;
+};
+
+// A word that an earlier launch wrote and this one only reads, at an address that
+// a wave's lanes share: a scalar load into a scalar register.
+__device__ inline int32_t scalar_word(const void* p, size_t i) {
+  return ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)p)[i];
+}
+__device__ inline Item scalar_item(const void* items, size_t i) {
+  Item it;
+  it.q0 = scalar_word(items, 8 * i); it.r0 = scalar_word(items, 8 * i + 1);
+  it.nr = scalar_word(items, 8 * i + 2); it.seq = scalar_word(items, 8 * i + 3);
+  it.k0 = scalar_word(items, 8 * i + 4); it.k1 = scalar_word(items, 8 * i + 5);
+  it.part = scalar_word(items, 8 * i + 6); it.pad = 0;
+  return it;
+}
+
+__device__ inline SeqInfo scalar_info(const void* infos, size_t i) {
+  SeqInfo f;
+  f.qoff = scalar_word(infos, 16 * i); f.open = scalar_word(infos, 16 * i + 1);
+  f.rows = scalar_word(infos, 16 * i + 2); f.share = scalar_word(infos, 16 * i + 3);
+  f.step = scalar_word(infos, 16 * i + 4); f.own_part = scalar_word(infos, 16 * i + 5);
+  f.own_chunks = scalar_word(infos, 16 * i + 6); f.own_blocks = scalar_word(infos, 16 * i + 7);
+  f.grp_part = scalar_word(infos, 16 * i + 8); f.grp_chunks = scalar_word(infos, 16 * i + 9);
+  f.grp_blocks = scalar_word(infos, 16 * i + 10); f.grp_off = scalar_word(infos, 16 * i + 11);
+  return f;
+}
+
+// Whether the workspace holds this handle's plan of the cache's present state for
+// these sizes; a workgroup that finds none records it and leaves, before it follows a
+// word of the plan. The handle's number stands for the layout of the workspace and of
+// the cache: another cache may have counted as many changes.
+__device__ inline bool plan_ok(const AttendArgs& a, int items) {
+  const bool ok = scalar_word(a.ws, 0) == scalar_word(a.p.state, kPagesVersion) &&
+                  scalar_word(a.ws, 1) == a.hq && scalar_word(a.ws, 2) == a.max_new &&
+                  scalar_word(a.ws, 4) == a.p.id &&
+                  items >= 0 && items <= a.w.max_items;
+  if (!ok && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.p.state + kPagesFlags, kFlagPlan);
+  return ok;
+}
+
+// The larger (the sum) of a lane's value and that of the lane 32 away.
+__device__ inline float other_half(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+__device__ inline float half_max(float x) { return fmaxf(x, other_half(x)); }
+__device__ inline float half_sum(float x) { return x + other_half(x); }
+
+// What scales the results so far from their maximum m to another, mu = max c2. The
+// product is rounded as mu was: fused with the difference it would leave mu's rounding
+// error where the maximum stays, and every step would scale by it (fp32, 512 rows, each
+// over 16384 keys of the score 7055: their mean off by 3.6e-3 instead of 1.7e-6).
+__device__ inline float rescale(float m, float c2, float mu) {
+#pragma clang fp contract(off)
+  return __builtin_amdgcn_exp2f(m * c2 - mu);
+}
+
+// The value of the column 16, 8, 4, 2 or 1 to the side, of the same half. By turns
+// for 8 and 4: of columns that agree at twice the distance, that is the same.
+template <int OFF> __device__ inline float aside(float x) {
+  const int v = __float_as_int(x);
+  if constexpr (OFF == 16) return __int_as_float(__builtin_amdgcn_ds_swizzle(v, 0x401f));
+  else return __int_as_float(__builtin_amdgcn_update_dpp(
+      0, v, OFF == 8 ? 0x128 : OFF == 4 ? 0x124 : OFF == 2 ? 0x4e : 0xb1, 0xf, 0xf, true));
+}
+
+// V where a mask crosses a step: keys from k1 on hold anything and count as 0. A
+// value that is not finite but masked for some rows only would reach them as
+// 0 x inf: it is taken out here (true: there was one), to be added to the rows
+// that see it when they are written. `k`: the key of the fragment's first element.
+template <typename T> __device__ inline bool clean_values(u32x4& v, int k, int k1) {
+  constexpr int E = Mma<T>::E;
+#pragma unroll
+  for (int j = 0; j < E; ++j)
+    if (k + j >= k1) {
+      if constexpr (E == 8) v[j >> 1] &= j & 1 ? 0x0000ffffu : 0xffff0000u;
+      else v[j] = 0u;
+    }
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    const bool inf = !(fabsf(Mma<T>::get(v, j)) < INFINITY);
+    bad = bad || inf;
+    if constexpr (E == 8) v[j >> 1] &= !inf ? 0xffffffffu : j & 1 ? 0x0000ffffu : 0xffff0000u;
+    else v[j] = inf ? 0u : v[j];
+  }
+  return bad;
+}
+
+// A block's partial results: O^T as the matrix products leave it, 16 bytes a lane
+// behind one another, and (m, l) of its rows. m is in units of the scores.
+template <int D> __device__ inline float* part_o(const AttendArgs& a, int head, long block) {
+  return reinterpret_cast<float*>(a.ws + a.w.o) + (head * a.w.blocks + block) * kBlock * D;
+}
+__device__ inline float2* part_ml(const AttendArgs& a, int head, long block) {
+  return reinterpret_cast<float2*>(a.ws + a.w.ml) + (head * a.w.blocks + block) * kBlock;
+}
+
+// Into a wave's o, m and l (column col: row it.r0 + col of sequence it.seq): the parts of
+// its rows, which W waves take in turn; l in the first half alone.
+template <int D, int W>
+__device__ inline void join_parts(const AttendArgs& a, const Item& it, const SeqInfo& f, int head,
+                                  int wave, float c2, f32x16 (&o)[D / 32], float& m, float& l) {
+  constexpr int ND = D / 32;
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  // parts: the group's chunks, then the tile's own. Of few rows there are columns
+  // to spare: R a part, and 32 / R parts at a time (4 rows of 32 parts, as 64
+  // sequences with one token each have, took 8 loads behind one another, 11 us).
+  const int t = it.r0 / tile_of(a.s).rows * tile_of(a.s).rows;
+  const int own = f.own_chunks ? ceil_div(tile_keys(f.rows, f.open, f.share, t, a.rep,
+                                                    tile_of(a.s).unit), f.step) : 0;
+  const int parts = f.grp_chunks + own;
+  int R = 32;
+  while (R > 1 && 2 * it.nr <= R && W * 32 < parts * R) R >>= 1;
+  const int rp = it.r0 + min(col & (R - 1), it.nr - 1), gr = f.grp_off + rp;
+  for (int c = wave + W * (col / R); c < parts; c += W * (32 / R)) {
+    const bool g = c < f.grp_chunks;
+    const long block = g ? f.grp_part + (long)c * f.grp_blocks + gr / kBlock
+                         : f.own_part + (long)(c - f.grp_chunks) * f.own_blocks + it.r0 / kBlock;
+    const int at = g ? gr % kBlock : rp % kBlock;
+    const float2 ml = part_ml(a, head, block)[at];
+    const float4* po = reinterpret_cast<const float4*>(part_o<D>(a, head, block)) + half * 32 + at;
+    float4 v[D / 8];
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) v[i] = po[i * 64];
+    const float mn = fmaxf(m, ml.x), mu = mn == -INFINITY ? 0.f : mn;
+    const float wo = __builtin_amdgcn_exp2f((m - mu) * c2);
+    const float wp = __builtin_amdgcn_exp2f((ml.x - mu) * c2);
+    m = mn;
+    l = l * wo + ml.y * wp;
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {
+      const int dt = i / 4, q = i % 4 * 4;
+      o[dt][q] = o[dt][q] * wo + v[i].x * wp;
+      o[dt][q + 1] = o[dt][q + 1] * wo + v[i].y * wp;
+      o[dt][q + 2] = o[dt][q + 2] * wo + v[i].z * wp;
+      o[dt][q + 3] = o[dt][q + 3] * wo + v[i].w * wp;
+    }
+  }
+  if (R < 32) {            // the columns of a row, to their common maximum and added up
+    float mn = fmaxf(m, aside<16>(m));
+    if (R < 16) mn = fmaxf(mn, aside<8>(mn));
+    if (R < 8) mn = fmaxf(mn, aside<4>(mn));
+    if (R < 4) mn = fmaxf(mn, aside<2>(mn));
+    if (R < 2) mn = fmaxf(mn, aside<1>(mn));
+    const float w = __builtin_amdgcn_exp2f((m - (mn == -INFINITY ? 0.f : mn)) * c2);
+    m = mn;
+    l *= w;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) o[dt] *= w;
+    auto add = [&](auto off) {
+      constexpr int OFF = decltype(off)::value;
+      l += aside<OFF>(l);
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] += aside<OFF>(o[dt][i]);
+    };
+    add(std::integral_constant<int, 16>{});
+    if (R < 16) add(std::integral_constant<int, 8>{});
+    if (R < 8) add(std::integral_constant<int, 4>{});
+    if (R < 4) add(std::integral_constant<int, 2>{});
+    if (R < 2) add(std::integral_constant<int, 1>{});
+  }
+  l = half ? 0.f : l;      // of both halves; the steps' sums are of one each
+}
+
+// The maximum that is taken out of a row's exponents follows the scores only when they
+// pass it by 2^kLazy, and is a whole power of two in the base of the exponential.
+constexpr float kLazy = 8.f;
+
+// The chunk of row r lies at its own number with these bits flipped, rows of C
+// chunks: 16 rows then have 16 places mod 256 bytes.
+template <int C> __device__ inline int turn(int r) {
+  static_assert(C == 16 || C == 8, "rows of 256 or 128 bytes");
+  return C == 16 ? r & 15 : (r >> 1) & 7;
+}
+}  // namespace
+}  // namespace ldr
+#endif

@@ -178,13 +178,16 @@ hipError_t launch_views_fork(const Shape& s, const Layout& L, int batch, void* a
 // table, refs, then scratch of the calls (lists of pages).
 struct PagesShape {
   int layers, hkv, d, page, n_pages, batch, max_pages, dtype;
-  size_t el;
-  size_t page_bytes;                 // one page of one layer's K (or V), all heads
+  int bits;                          // of a code; 0: rows of the dtype
+  size_t el;                         // bytes of an element of the rows outside the pool
+  size_t head_bytes;                 // one head's rows in a page of one layer's K (or V)
+  size_t page_bytes;                 // all heads' of them
   size_t rows, open, table, refs;    // word offsets in the state
   size_t list;                       // scratch: n_pages words (free pages; compaction map)
   size_t pairs;                      // scratch: 2 max(batch, n_pages / 2 + 1) words (from, to)
   size_t words;
 };
+constexpr int kMxBlock = 32;      // dimensions that share a scale in a coded cache
 // Header words of the state.
 constexpr int kPagesFlags = 0;    // sticky flags
 constexpr int kPagesVersion = 1;  // counts the calls that change the tables, resets too
@@ -200,6 +203,11 @@ hipError_t launch_pages_reserve(const PagesShape& s, const PagesPtrs& p, const i
                                 int max_new, hipStream_t st);
 hipError_t launch_pages_write(const PagesShape& s, const PagesPtrs& p, int layer, int n_layers,
                               const void* K, const void* V, int max_new, hipStream_t st);
+hipError_t launch_pages_write_mx(const PagesShape& s, const PagesPtrs& p, int layer, int n_layers,
+                                 const void* K, const void* V, int max_new, hipStream_t st);
+hipError_t launch_pages_read(const PagesShape& s, const PagesPtrs& p, int layer, int n_layers,
+                             const int32_t* first, const int32_t* n, void* K, void* V,
+                             int max_rows, hipStream_t st);
 hipError_t launch_pages_keep(const PagesShape& s, const PagesPtrs& p, const int32_t* kept,
                              hipStream_t st);
 hipError_t launch_pages_fork(const PagesShape& s, const PagesPtrs& p, const int32_t* src,
@@ -215,6 +223,10 @@ hipError_t launch_attend_plan(const PagesShape& s, const PagesPtrs& p, int hq, i
 hipError_t launch_attend(const PagesShape& s, const PagesPtrs& p, int layer, const void* q,
                          long q_stride, int hq, int max_new, float scale, void* o, float* lse,
                          void* ws, hipStream_t st);
+// over coded rows (attend_mx.hip)
+hipError_t launch_attend_mx(const PagesShape& s, const PagesPtrs& p, int layer, const void* q,
+                            long q_stride, int hq, int max_new, float scale, void* o, float* lse,
+                            void* ws, hipStream_t st);
 
 // Verification from given probabilities and uniforms (verify_probs.hip).
 size_t verify_probs_workspace_bytes(int batch, int B, int V);
@@ -222,6 +234,13 @@ hipError_t launch_verify_probs(const float* P, const float* Q, const int32_t* y,
                                const int32_t* n_draft, const float* u, int batch, int B, int V,
                                int32_t* accepted, int32_t* token, int32_t* n_new, void* ws,
                                hipStream_t st);
+
+// Log probabilities of given tokens (logprobs.hip).
+size_t logprobs_workspace_bytes(int batch, int rows, int vocab, int top);
+hipError_t launch_logprobs(const float* logits, int64_t stride, const int32_t* tokens,
+                           const int32_t* n_rows, int batch, int rows, int vocab,
+                           float temperature, int top, float* logp, float* entropy, int32_t* rank,
+                           int32_t* top_tokens, float* top_logp, void* ws, hipStream_t st);
 
 // GEMM (gemm.hip): C = A[M][K] . W[N][K]^T, fp32 accumulation.
 enum GemmEpi {

@@ -1,0 +1,307 @@
+// Log probabilities of given tokens, the entropy of their rows, the tokens' ranks, and
+// the rows' largest entries.
+//
+// With m the largest logit of a row, x_v = (z_v - m) / T and S = sum e^{x_v}, which is the
+// number of entries equal to m plus the rest R:
+//   log p(v) = x_v - log S,  entropy = log S - sum e^{x_v} x_v / S,  log S = log1p(S - 1),
+// so that a nearly certain token keeps its digits. One pass over the logits cuts a row
+// into pieces; a piece stays in registers while its m, and then its sums, are taken, and it
+// counts the entries that rank before the token. A second launch joins the pieces of a row.
+//
+// The n largest entries are among the n groups of 64 neighbours with the largest maxima (in
+// the order by value, then by index: a group that is not has n entries before any of its
+// own). The first pass writes the maxima; the second picks the groups, then the entries in
+// them, with sorted lists of 64 keys across the lanes of a wave.
+//
+// Bound by the one read of the logits.
+#include "ldr_internal.h"
+
+namespace ldr {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kGroup = 64;        // neighbours that share a maximum
+constexpr int kWaves = 16;        // of a workgroup that picks entries
+constexpr int kMostTop = 64;
+
+// An exponent whose power is 0: -inf times that is to be 0 too.
+constexpr float kFar = -1e4f;
+struct __attribute__((packed, aligned(4))) Four { float x[4]; };   // rows may start anywhere
+
+// A piece of a row: its maximum, how many entries equal it, the others' sum of e^x and the
+// sum of e^x x (x of base 2), and the entries that rank before the token.
+struct Piece { float m, rest, ex; int ones, before; };
+
+struct LogprobsArgs {
+  const float* z; long stride;
+  const int32_t* tokens; const int32_t* n_rows;
+  int rows, vocab, pieces, groups, top;
+  float temperature, c;           // c: log2(e) / T
+  float *logp, *entropy; int32_t* rank; int32_t* top_tokens; float* top_logp;
+  Piece* parts; uint32_t* maxima;
+};
+
+// Larger entries have larger keys; a NaN's is the lowest.
+__device__ inline uint32_t key_of(float z) { return z == z ? order_key(z) : 0u; }
+
+__device__ inline float wave_max(float v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
+  return v;
+}
+template <typename T> __device__ inline T wave_sum(T v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
+  return v;
+}
+
+// One piece of 1024 U entries: thread t has four of every 1024.
+template <int U, bool TOP>
+__global__ void __launch_bounds__(kThreads) logprobs_pieces_kernel(LogprobsArgs a) {
+  constexpr int W = kThreads / 64;
+  __shared__ float sm[W], srest[W], sex[W];
+  __shared__ int sones[W], sbefore[W];
+  const int b = blockIdx.z, i = blockIdx.y, piece = blockIdx.x;
+  if (a.n_rows && i >= a.n_rows[b]) return;
+  const size_t row = (size_t)b * a.rows + i;
+  const float* z = a.z + row * a.stride;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int first = piece * (1024 * U) + (int)threadIdx.x * 4;
+  const int y = a.tokens[row];
+  const bool given = y >= 0 && y < a.vocab;
+  const float zy = given ? z[y] : NAN;
+  float v[U][4];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int at = first + u * 1024;
+    if (at + 4 <= a.vocab) {
+      const Four f = *reinterpret_cast<const Four*>(z + at);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[u][k] = f.x[k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[u][k] = at + k < a.vocab ? z[at + k] : -INFINITY;
+    }
+  }
+  float m = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int at = first + u * 1024;
+    float g = NAN;            // stays where all are NaN
+#pragma unroll
+    for (int k = 0; k < 4; ++k) g = fmaxf(g, at + k < a.vocab ? v[u][k] : NAN);
+    m = fmaxf(m, g);
+    if constexpr (TOP) {      // a group is the entries of 16 lanes
+      const float most = max16(g);
+      if (lane % 16 == 0 && at < a.vocab) a.maxima[row * a.groups + at / kGroup] = key_of(most);
+    }
+  }
+  m = wave_max(m);
+  if (lane == 0) sm[wave] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < W; ++w) m = fmaxf(m, sm[w]);
+  const float base = m == -INFINITY ? 0.f : m;
+  float rest = 0.f, ex = 0.f;
+  int ones = 0, before = 0;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float w = v[u][k], x = (w - base) * a.c, e = __builtin_amdgcn_exp2f(x);
+      ones += __builtin_popcountll(__ballot(w == m));
+      rest += w == m ? 0.f : e;
+      ex = fmaf(e, fmaxf(x, kFar), ex);       // of -inf: 0
+      before += w > zy || (w == zy && first + u * 1024 + k < y);
+    }
+  if (zy != zy && given) {                      // behind every number
+    before = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int at = first + u * 1024 + k;
+        before += at < a.vocab && (v[u][k] == v[u][k] || at < y);
+      }
+  }
+  rest = wave_sum(rest);
+  ex = wave_sum(ex);
+  before = wave_sum(before);
+  if (lane == 0) { srest[wave] = rest; sex[wave] = ex; sones[wave] = ones; sbefore[wave] = before; }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    Piece p{m, 0.f, 0.f, 0, 0};
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      p.rest += srest[w]; p.ex += sex[w]; p.ones += sones[w]; p.before += sbefore[w];
+    }
+    a.parts[row * a.pieces + piece] = p;
+  }
+}
+
+// Keys across a wave, the largest in lane 0.
+struct Key { uint32_t hi, lo; };     // the value's key, the index's complement
+__device__ inline bool ahead(const Key& a, const Key& b) {
+  return a.hi > b.hi || (a.hi == b.hi && a.lo > b.lo);
+}
+__device__ inline Key from_lane(const Key& k, int mask) {
+  return Key{(uint32_t)__shfl_xor((int)k.hi, mask), (uint32_t)__shfl_xor((int)k.lo, mask)};
+}
+// The larger (or the smaller) of a lane's key and that of the lane `mask` away.
+__device__ inline void exchange(Key& k, int mask, bool larger) {
+  const Key o = from_lane(k, mask);
+  if (ahead(o, k) == larger) k = o;
+}
+__device__ inline void sort64(Key& k) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int size = 2; size <= 64; size <<= 1)
+#pragma unroll
+    for (int off = size >> 1; off >= 1; off >>= 1)
+      exchange(k, off, ((lane & off) == 0) == ((lane & size) == 0));
+}
+// The 64 largest of two sorted lists, `o` turned round (lane l has its entry 63 - l).
+__device__ inline void merge64(Key& k, const Key& o) {
+  const int lane = threadIdx.x & 63;
+  if (ahead(o, k)) k = o;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) exchange(k, off, (lane & off) == 0);
+}
+// Up to 64 more keys into a wave's list, of which the first n count.
+__device__ inline void add64(Key& list, Key k, int n) {
+  const Key last{(uint32_t)__shfl((int)list.hi, n - 1), (uint32_t)__shfl((int)list.lo, n - 1)};
+  if (!__any(ahead(k, last))) return;
+  sort64(k);
+  merge64(list, from_lane(k, 63));
+}
+// The waves' lists into one that all of them have; `lds`: 64 a wave.
+__device__ inline void join_lists(Key& list, Key* lds, int lane, int wave) {
+  __syncthreads();
+  lds[wave * 64 + lane] = list;
+#pragma unroll
+  for (int n = kWaves / 2; n >= 1; n >>= 1) {
+    __syncthreads();
+    if (wave < n) {
+      merge64(list, lds[(wave + n) * 64 + 63 - lane]);
+      lds[wave * 64 + lane] = list;
+    }
+  }
+  __syncthreads();
+  list = lds[lane];
+}
+
+// The pieces of a row, and what is left of each row's answer.
+template <bool TOP>
+__global__ void __launch_bounds__(TOP ? kWaves * 64 : 64) logprobs_rows_kernel(LogprobsArgs a) {
+  __shared__ Key lists[TOP ? kWaves * 64 : 1];
+  const int b = blockIdx.y, i = blockIdx.x;
+  if (a.n_rows && i >= a.n_rows[b]) return;
+  const size_t row = (size_t)b * a.rows + i;
+  const float* z = a.z + row * a.stride;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Piece* parts = a.parts + row * a.pieces;
+  const int y = a.tokens[row];
+  const bool given = y >= 0 && y < a.vocab;
+  const float zy = given ? z[y] : -INFINITY;
+  float m = -INFINITY;
+  for (int p = lane; p < a.pieces; p += 64) m = fmaxf(m, parts[p].m);
+  m = wave_max(m);
+  const float base = m == -INFINITY ? 0.f : m;
+  float rest = 0.f, ex = 0.f;
+  int ones = 0, before = 0;
+  for (int p = lane; p < a.pieces; p += 64) {
+    const Piece q = parts[p];
+    const float x = (q.m - base) * a.c, w = __builtin_amdgcn_exp2f(x);
+    if (q.m == m) ones += q.ones;
+    else rest += w * q.ones;
+    rest += w * q.rest;
+    ex += w * fmaf(q.rest + q.ones, fmaxf(x, kFar), q.ex);
+    before += q.before;
+  }
+  rest = wave_sum(rest);
+  ex = wave_sum(ex);
+  ones = wave_sum(ones);
+  before = wave_sum(before);
+  if (m == INFINITY) rest = NAN;
+  const bool empty = m == -INFINITY && rest == 0.f;       // every entry is -inf
+  const float more = (float)(ones - 1) + rest, ls = log1pf(more);
+  auto logp = [&](float v) {
+    return empty || v == -INFINITY ? (rest == rest ? -INFINITY : rest) : (v - base) / a.temperature - ls;
+  };
+  if (threadIdx.x == 0) {
+    a.logp[row] = given ? logp(zy) : rest == rest ? -INFINITY : rest;
+    a.entropy[row] = empty ? 0.f : ls - ex / (more + 1.f) * 0.693147180559945309f;
+    a.rank[row] = given ? before : a.vocab;
+  }
+  if constexpr (TOP) {
+    // groups, then the entries of the first `top` of them
+    Key list{0u, 0u};
+    const uint32_t* maxima = a.maxima + row * a.groups;
+    for (int g0 = wave * 64; g0 < a.groups; g0 += kWaves * 64) {
+      const int g = g0 + lane;
+      add64(list, g < a.groups ? Key{maxima[g], ~(uint32_t)g} : Key{0u, 0u}, a.top);
+    }
+    join_lists(list, lists, lane, wave);
+    Key best{0u, 0u};
+    const int n = min(a.top, a.groups);
+    for (int j = wave; j < n; j += kWaves) {
+      const uint32_t g = ~(uint32_t)__shfl((int)list.lo, j);
+      const int v = (int)g * kGroup + lane;
+      add64(best, v < a.vocab ? Key{key_of(z[v]), ~(uint32_t)v} : Key{0u, 0u}, a.top);
+    }
+    join_lists(best, lists, lane, wave);
+    if (wave == 0 && lane < a.top) {
+      const int v = (int)~best.lo;
+      a.top_tokens[row * a.top + lane] = v;
+      a.top_logp[row * a.top + lane] = logp(z[v]);
+    }
+  }
+}
+
+// Entries of a piece: enough pieces to fill the GPU, or as many loads in flight.
+int units_of(int64_t rows, int vocab) {
+  return rows * ((vocab + 8191) / 8192) >= 512 ? 8 : 2;
+}
+int pieces_of(int64_t rows, int vocab) {
+  const int n = 1024 * units_of(rows, vocab);
+  return (vocab + n - 1) / n;
+}
+
+template <int U> void launch_pieces(const LogprobsArgs& a, int batch, hipStream_t st) {
+  const dim3 grid(a.pieces, a.rows, batch);
+  if (a.top)
+    hipLaunchKernelGGL((logprobs_pieces_kernel<U, true>), grid, dim3(kThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((logprobs_pieces_kernel<U, false>), grid, dim3(kThreads), 0, st, a);
+}
+
+}  // namespace
+
+size_t logprobs_workspace_bytes(int batch, int rows, int vocab, int top) {
+  const int64_t n = (int64_t)batch * rows;
+  return align_up(n * pieces_of(n, vocab) * sizeof(Piece)) +
+         (top ? align_up(n * ((vocab + kGroup - 1) / kGroup) * 4) : 0);
+}
+
+hipError_t launch_logprobs(const float* logits, int64_t stride, const int32_t* tokens,
+                           const int32_t* n_rows, int batch, int rows, int vocab,
+                           float temperature, int top, float* logp, float* entropy, int32_t* rank,
+                           int32_t* top_tokens, float* top_logp, void* ws, hipStream_t st) {
+  const int64_t n = (int64_t)batch * rows;
+  LogprobsArgs a{logits, (long)stride, tokens, n_rows, rows, vocab, pieces_of(n, vocab),
+                 (vocab + kGroup - 1) / kGroup, top, temperature, kLog2e / temperature,
+                 logp, entropy, rank, top_tokens, top_logp, static_cast<Piece*>(ws), nullptr};
+  a.maxima = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(ws) +
+                                         align_up(n * a.pieces * sizeof(Piece)));
+  if (units_of(n, vocab) == 8) launch_pieces<8>(a, batch, st);
+  else launch_pieces<2>(a, batch, st);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (top)
+    hipLaunchKernelGGL(logprobs_rows_kernel<true>, dim3(rows, batch), dim3(kWaves * 64), 0, st, a);
+  else
+    hipLaunchKernelGGL(logprobs_rows_kernel<false>, dim3(rows, batch), dim3(64), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace ldr

@@ -398,6 +398,7 @@ hipError_t launch_pages_write(const PagesShape& s, const PagesPtrs& p, int layer
                               const void* K, const void* V, int max_new, hipStream_t st) {
   // tiles begin at a multiple of 16 bytes, up to a run less one before the rows
   const dim3 grid((max_new + 16 / (int)s.el + 30) / 32, n_layers * s.hkv, s.batch);
+  if (s.bits) return launch_pages_write_mx(s, p, layer, n_layers, K, V, max_new, st);
   if (s.dtype == LDR_BF16)
     hipLaunchKernelGGL(pages_write_kernel<uint16_t>, grid, dim3(kThreads), 0, st, s, p, layer,
                        n_layers, static_cast<const uint16_t*>(K),

@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libldr.so")
 LDR_OK, LDR_EINVAL, LDR_ERANGE, LDR_EHIP, LDR_ENOMEM, LDR_ESCRATCH = 0, -1, -2, -3, -4, -5
 LDR_EPAGES = -6
 NOALLOC_SCRATCH_BYTES = 16 << 20   # LDR_NOALLOC_SCRATCH_BYTES
-LDR_F32, LDR_BF16 = 0, 1
+LDR_F32, LDR_BF16, LDR_MXFP4, LDR_MXFP8 = 0, 1, 4, 8
 
 
 class LdrError(RuntimeError):
@@ -113,6 +113,7 @@ def _lib():
             "ldr_pages_init": (ctypes.c_int, [ctypes.POINTER(P), PP, P, P, P]),
             "ldr_pages_reserve": (ctypes.c_int, [P, P, I32, P]),
             "ldr_pages_write": (ctypes.c_int, [P, I32, I32, P, P, I32, P]),
+            "ldr_pages_read": (ctypes.c_int, [P, I32, I32, P, P, P, P, I32, P]),
             "ldr_pages_keep": (ctypes.c_int, [P, P, P]),
             "ldr_pages_fork": (ctypes.c_int, [P, P, P]),
             "ldr_pages_compact": (ctypes.c_int, [P, P]),
@@ -124,6 +125,9 @@ def _lib():
                                           P]),
             "ldr_verify_probs_workspace_bytes": (SZ, [I32, I32, I32]),
             "ldr_verify_probs": (ctypes.c_int, [P, P, P, P, P, I32, I32, I32, P, P, P, P, SZ, P]),
+            "ldr_logprobs_workspace_bytes": (SZ, [I32, I32, I32, I32]),
+            "ldr_logprobs": (ctypes.c_int, [P, I64, P, P, I32, I32, I32, ctypes.c_float, I32, P, P,
+                                            P, P, P, P, SZ, P]),
             "ldr_strerror": (ctypes.c_char_p, [ctypes.c_int]),
         }
         for name, (res, args) in sig.items():
@@ -627,23 +631,35 @@ class Pages:
     rows, open [batch], table [batch][max_pages] and refs [n_pages] are int32
     views of `state`; `pool` is [n_layers][2][n_pages][n_kv_heads][page *
     head_dim]. A clone of `state` copied back later undoes the calls in between
-    for the tables (not for the pool)."""
+    for the tables (not for the pool).
+
+    codes = "mxfp8" or "mxfp4": the pool holds bf16 rows as codes of 8 or 4 bits (LDR_MXFP8,
+    LDR_MXFP4), uint8 [n_layers][2][n_pages][n_kv_heads][bytes of a head's rows]; rows in
+    and out stay bf16."""
 
     def __init__(self, n_layers: int, n_kv_heads: int, head_dim: int, page: int, n_pages: int,
                  batch: int, max_pages: int, dtype: torch.dtype = torch.bfloat16, device="cuda",
-                 stream=None):
+                 stream=None, codes: Optional[str] = None):
         if dtype not in (torch.bfloat16, torch.float32):
             raise LdrError(LDR_EINVAL, f"a cache of {dtype}")
+        if codes not in (None, "mxfp8", "mxfp4") or (codes and dtype != torch.bfloat16):
+            raise LdrError(LDR_EINVAL, f"a cache of {dtype} in codes {codes}")
+        held = {None: LDR_BF16 if dtype == torch.bfloat16 else LDR_F32, "mxfp8": LDR_MXFP8,
+                "mxfp4": LDR_MXFP4}[codes]
         self.cfg = PagesConfig(n_layers, n_kv_heads, head_dim, page, n_pages, batch, max_pages,
-                               LDR_BF16 if dtype == torch.bfloat16 else LDR_F32)
+                               held)
         L = _lib()
         words = L.ldr_pages_state_bytes(ctypes.byref(self.cfg)) // 4
         if not words:
             raise LdrError(LDR_EINVAL, "Pages")
         self.batch, self.page, self.n_pages, self.max_pages = batch, page, n_pages, max_pages
         self.n_layers, self.hkv, self.d, self.dtype = n_layers, n_kv_heads, head_dim, dtype
-        self.pool = torch.empty(n_layers, 2, n_pages, n_kv_heads, page * head_dim, dtype=dtype,
-                                device=device)
+        self.codes = codes
+        pool = L.ldr_pages_pool_bytes(ctypes.byref(self.cfg))
+        held = torch.uint8 if codes else dtype
+        self.pool = torch.empty(n_layers, 2, n_pages, n_kv_heads,
+                                pool // (2 * n_layers * n_pages * n_kv_heads * held.itemsize),
+                                dtype=held, device=device)
         self.device = self.pool.device
         self.state = torch.empty(words, dtype=torch.int32, device=device)
         off = (ctypes.c_size_t * 4)()
@@ -672,12 +688,18 @@ class Pages:
         return _stream(self._stream, self.device)
 
     def k(self, layer: int) -> torch.Tensor:
-        """A layer's K pages [n_pages][n_kv_heads][page][head_dim]."""
+        """A layer's K pages [n_pages][n_kv_heads][page][head_dim] (not of a coded cache: read)."""
+        self._plain("k")
         return self.pool[layer, 0].view(self.n_pages, self.hkv, self.page, self.d)
 
     def v(self, layer: int) -> torch.Tensor:
-        """A layer's V pages, transposed [n_pages][n_kv_heads][head_dim][page]."""
+        """A layer's V pages, transposed [n_pages][n_kv_heads][head_dim][page] (as k)."""
+        self._plain("v")
         return self.pool[layer, 1].view(self.n_pages, self.hkv, self.d, self.page)
+
+    def _plain(self, what: str):
+        if self.codes:
+            raise LdrError(LDR_EINVAL, f"Pages.{what} of a cache in codes {self.codes}")
 
     def reserve(self, n_new: torch.Tensor, max_new: int):
         """ldr_pages_reserve: room for n_new[b] more rows (int32 [batch], at most
@@ -701,6 +723,32 @@ class Pages:
             raise LdrError(LDR_EINVAL, f"append of K {tuple(K.shape)}")
         self.reserve(n_new, K.shape[1])
         self.write(K, V)
+
+    def read(self, first: torch.Tensor, n: torch.Tensor, max_rows: Optional[int] = None,
+             layer: int = 0, n_layers: Optional[int] = None, out=None):
+        """ldr_pages_read: rows first[b] .. first[b] + n[b] - 1 (int32 [batch]) of layers
+        `layer` and on, as (K, V) [batch][max_rows][layers][n_kv_heads][head_dim]; rows
+        behind n[b] stay as they are (0 in new ones). With `out`, its sizes count."""
+        _take(first, (self.batch,), torch.int32, self.device, "first")
+        _take(n, (self.batch,), torch.int32, self.device, "n")
+        if out is None:
+            if max_rows is None:
+                raise LdrError(LDR_EINVAL, "Pages.read without max_rows or out")
+            n_layers = self.n_layers - layer if n_layers is None else n_layers
+            shape = (self.batch, max_rows, n_layers, self.hkv, self.d)
+            if min(shape) < 1:
+                raise LdrError(LDR_EINVAL, f"Pages.read of {shape}")
+            with _on(self._stream):
+                out = tuple(torch.zeros(shape, dtype=self.dtype, device=self.device)
+                            for _ in range(2))
+        K, V = out
+        shape = ((self.batch, max_rows or K.shape[1], n_layers or K.shape[2], self.hkv, self.d)
+                 if K.dim() == 5 else ())
+        _take(K, shape, self.dtype, self.device, "K")
+        _take(V, shape, self.dtype, self.device, "V")
+        _check(_lib().ldr_pages_read(self._h, int(layer), shape[2], _ptr(first), _ptr(n), _ptr(K),
+                                     _ptr(V), shape[1], self._at()), "ldr_pages_read")
+        return K, V
 
     def keep(self, kept: torch.Tensor):
         """ldr_pages_keep: of the open rows, the first kept[b] (int32 [batch])."""
@@ -829,4 +877,55 @@ def verify_probs(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor]
                                    _ptr(n_draft), _ptr(uniforms), batch, B, V, _ptr(acc),
                                    _ptr(tok), _ptr(n_new), _ptr(workspace), workspace.numel(),
                                    _stream(stream, dev)), "ldr_verify_probs")
+    return out
+
+
+def logprobs_workspace_bytes(batch: int, rows: int, vocab: int, top_n: int) -> int:
+    return int(_lib().ldr_logprobs_workspace_bytes(batch, rows, vocab, top_n))
+
+
+def logprobs(logits: torch.Tensor, tokens: torch.Tensor, top_n: int = 0, temperature: float = 1.0,
+             n_rows: Optional[torch.Tensor] = None, out=None,
+             workspace: Optional[torch.Tensor] = None, stream=None):
+    """ldr_logprobs: fp32 logits [batch][rows][V], their rows a constant stride apart, and
+    tokens int32 [batch][rows] -> (logp, entropy fp32, rank int32 [batch][rows], top_tokens
+    int32, top_logp fp32 [batch][rows][top_n]). Rows behind n_rows[b] (int32 [batch]) stay
+    as they are (0 in new outputs)."""
+    if logits.dim() != 3:
+        raise LdrError(LDR_EINVAL, f"logits of {tuple(logits.shape)}")
+    batch, rows, V = logits.shape
+    dev = logits.device
+    # the stride of a row (b, i), whatever torch says of dimensions of one entry
+    row = logits.stride(1) if rows > 1 else logits.stride(0) if batch > 1 else V
+    if (logits.dtype != torch.float32 or (V > 1 and logits.stride(2) != 1)
+            or (rows > 1 and batch > 1 and logits.stride(0) != rows * row)):
+        raise LdrError(LDR_EINVAL, f"logits of {logits.dtype}, strides {logits.stride()}")
+    _take(tokens, (batch, rows), torch.int32, dev, "tokens")
+    if n_rows is not None:
+        _take(n_rows, (batch,), torch.int32, dev, "n_rows")
+    need = logprobs_workspace_bytes(batch, rows, V, int(top_n))
+    if not need:
+        raise LdrError(LDR_EINVAL, f"logprobs of {tuple(logits.shape)}, top_n {top_n}")
+    if out is None:
+        with _on(stream):
+            out = (torch.zeros(batch, rows, device=dev), torch.zeros(batch, rows, device=dev),
+                   torch.zeros(batch, rows, dtype=torch.int32, device=dev),
+                   torch.zeros(batch, rows, top_n, dtype=torch.int32, device=dev),
+                   torch.zeros(batch, rows, top_n, device=dev))
+    logp, entropy, rank, top_tokens, top_logp = out
+    for t, name, dtype, shape in ((logp, "logp", torch.float32, (batch, rows)),
+                                  (entropy, "entropy", torch.float32, (batch, rows)),
+                                  (rank, "rank", torch.int32, (batch, rows)),
+                                  (top_tokens, "top_tokens", torch.int32, (batch, rows, top_n)),
+                                  (top_logp, "top_logp", torch.float32, (batch, rows, top_n))):
+        _take(t, shape, dtype, dev, name)
+    if workspace is None:
+        with _on(stream):
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    _take(workspace, (workspace.numel(),), torch.uint8, dev, "workspace")
+    _on_gpu(dev, "logprobs")
+    _check(_lib().ldr_logprobs(_ptr(logits), row, _ptr(tokens), _ptr(n_rows), batch, rows, V,
+                               float(temperature), int(top_n), _ptr(logp), _ptr(entropy),
+                               _ptr(rank), _ptr(top_tokens), _ptr(top_logp), _ptr(workspace),
+                               workspace.numel(), _stream(stream, dev)), "ldr_logprobs")
     return out
