@@ -57,11 +57,24 @@ __device__ inline int even_step(int len, int n, int unit) {
   return ((len + n - 1) / n + unit - 1) / unit * unit;
 }
 
+// The time of an item of a coded cache, in sixteenths of a whole tile's, and the smallest
+// chunk (of the lightest items, tile.unit keys). Measured, 32 query and 8 K/V heads of 128,
+// 4 bits, all compute units at it, for 1024 keys: up to 32 rows 6.4 us, 64 10.9, 96 17.5,
+// 256 30.5. Without weights a batch whose sequences have 60, 64 and 68 rows took 71 us a
+// layer, of which 26 were for the workgroups of 68 alone.
+constexpr int kMxLeast = 48;
+__device__ inline int mx_weighted(int len, int rows) {
+  const int w = rows <= 32 ? 3 : rows <= 64 ? 6 : rows <= 96 ? 9 : rows <= 128 ? 11 : 16;
+  return (int)(((long)len * w + 15) / 16);
+}
+
 // The plan, in one workgroup: thread b has sequence b; what looks at all
 // sequences for each goes by waves, a sequence at a time. 5.7 us for one sequence, 23 for
 // 64 with 512 pages in common (their tables, 128 KB, through one compute unit): once
 // for all layers.
-template <bool BF16>
+// MX: a coded cache, whose items take as long as their rows ask for (mx_weight): a chunk is
+// as many sixteenths of a whole tile's keys.
+template <bool BF16, bool MX = false>
 __global__ void __launch_bounds__(kBook)
 attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t* groups,
                    uint8_t* ws, AttendWs w) {
@@ -82,6 +95,7 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   SeqInfo* info = reinterpret_cast<SeqInfo*>(ws + w.info);
   Item* items = reinterpret_cast<Item*>(ws + w.items);
   constexpr Tile tile = tile_of(BF16);   // divisions by its entries are shifts
+  constexpr int least_chunk = MX ? kMxLeast : tile.unit, quantum = MX ? 16 : tile.unit;
 
   const int all = in ? clamp_rows(s, p.state[s.rows + b]) : 0;
   const int held = in ? min(max(p.state[s.open + b], 0), all) : 0;
@@ -170,8 +184,10 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   o_len[b] = len;
   shares[b] = share;
   ends[b] = rows;
-  cuts[b] = float4{(float)ot, (float)len, (float)gt, (float)glen};
-  const float mine = wave_sum((float)ot * len + (float)gt * glen);
+  // what the chunks are cut by
+  const int wlen = MX ? mx_weighted(len, R) : len, wglen = MX ? mx_weighted(glen, Rg) : glen;
+  cuts[b] = float4{(float)ot, (float)wlen, (float)gt, (float)wglen};
+  const float mine = wave_sum((float)ot * wlen + (float)gt * wglen);
   if (lane == 0) works[wave] = mine;
   __syncthreads();
   // The chunk: a lane has a length, a wave some of the sequences. With slots for all
@@ -180,10 +196,10 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   float work = 0.f;
   for (int w = 0; w < NW; ++w) work += works[w];
   const float even = work * s.hkv / tile.slots;
-  const int least = max((int)min(even / kMaxRounds + 1.f, 1e8f), tile.unit);
+  const int least = max((int)min(even / kMaxRounds + 1.f, 1e8f), least_chunk);
   // from `least` to 4.5 x kMaxRounds of it, in even ratios
   const float x = least * __builtin_amdgcn_exp2f(lane * (3.2f / 64));
-  int chunk = ceil_div((int)x, tile.unit) * tile.unit;
+  int chunk = ceil_div((int)x, quantum) * quantum;
   {
     const float per = __builtin_amdgcn_rcpf((float)chunk);
     float n = 0.f;           // of chunks, nearly: for an estimate
@@ -206,7 +222,11 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
       if (oc < cost || (oc == cost && ch < chunk)) { cost = oc; chunk = ch; }
     }
   }
-  const int oc = (len + chunk - 1) / chunk, gc = (glen + chunk - 1) / chunk;
+  int oc = (wlen + chunk - 1) / chunk, gc = (wglen + chunk - 1) / chunk;
+  if (MX) {     // of whole units there may be fewer: none of the chunks is empty
+    if (oc) oc = ceil_div(len, even_step(len, oc, tile.unit));
+    if (gc) gc = ceil_div(glen, even_step(glen, gc, tile.unit));
+  }
   const int ob = ceil_div(R, kBlock), gb = ceil_div(Rg, kBlock);
   // the list: each sequence's own items, then its group's; and the blocks of parts
   // both counts in one scan: below 2^31 each, by the bound on the chunk
@@ -878,8 +898,10 @@ hipError_t launch_attend_plan(const PagesShape& s, const PagesPtrs& p, int hq, i
   // a wave a sequence: four waves share a SIMD, so that 16 make every step four times as
   // long (one sequence over 2048 keys, all launches: 20.9 us, 22.5 with 16)
   const int waves = min(max(s.batch, 4), kBook / 64);
-  hipLaunchKernelGGL(s.dtype != LDR_F32 ? attend_plan_kernel<true> : attend_plan_kernel<false>,
-                     dim3(1), dim3(64 * waves), 0, st, s, p, hq, max_new, groups,
+  const auto kernel = s.bits ? attend_plan_kernel<true, true>
+                      : s.dtype == LDR_BF16 ? attend_plan_kernel<true, false>
+                                            : attend_plan_kernel<false, false>;
+  hipLaunchKernelGGL(kernel, dim3(1), dim3(64 * waves), 0, st, s, p, hq, max_new, groups,
                      static_cast<uint8_t*>(ws), plan_ws(s, hq, max_new));
   return hipGetLastError();
 }
