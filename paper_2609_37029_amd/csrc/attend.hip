@@ -59,12 +59,11 @@ __device__ inline int even_step(int len, int n, int unit) {
 
 // The time of an item of a coded cache, in sixteenths of a whole tile's, and the smallest
 // chunk (of the lightest items, tile.unit keys). Measured, 32 query and 8 K/V heads of 128,
-// 4 bits, all compute units at it, for 1024 keys: up to 32 rows 6.4 us, 64 10.9, 96 17.5,
-// 256 30.5. Without weights a batch whose sequences have 60, 64 and 68 rows took 71 us a
-// layer, of which 26 were for the workgroups of 68 alone.
+// 4 bits, all compute units at it, for 1024 keys: up to 32 rows 6.4 us, 64 9.3, 128 17.3,
+// 256 29.4; of 65 to 96 rows two tiles, 4 sixteenths each.
 constexpr int kMxLeast = 48;
 __device__ inline int mx_weighted(int len, int rows) {
-  const int w = rows <= 32 ? 3 : rows <= 64 ? 6 : rows <= 96 ? 9 : rows <= 128 ? 11 : 16;
+  const int w = rows <= 32 ? 3 : rows <= 64 ? 5 : rows <= 96 ? 4 : rows <= 128 ? 9 : 16;
   return (int)(((long)len * w + 15) / 16);
 }
 
@@ -177,8 +176,9 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   const int share = in && members[b] > 1 && common_rows >= kMinShared ? common_rows : 0;
   const int gopen = in ? gopens[b] : 0;
   const int R = open * rep, Rg = share && ld == b ? gopen * rep : 0;    // below 2^28
-  const int ot = ceil_div(R, tile.rows), gt = ceil_div(Rg, tile.rows);
-  int len = open ? tile_keys(rows, open, share, (ot - 1) * tile.rows, rep, tile.unit) : 0;
+  const int otr = tile_rows(tile, MX, R), ot = ceil_div(R, otr);
+  const int gt = ceil_div(Rg, tile_rows(tile, MX, Rg));
+  int len = open ? tile_keys(rows, open, share, (ot - 1) * otr, rep, tile.unit) : 0;
   if (len < kMinMain) len = 0;
   const int glen = Rg ? share : 0;
   o_len[b] = len;
@@ -274,13 +274,14 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
       const int mid = (lo + hi + 1) >> 1;
       if (i_off[mid] <= t) lo = mid; else hi = mid - 1;
     }
-    const int own_rows = opens[lo] * rep, own_tiles = (own_rows + tile.rows - 1) / tile.rows;
+    const int own_rows = opens[lo] * rep;
+    const int own_tiles = ceil_div(own_rows, tile_rows(tile, MX, own_rows));
     int k = t - i_off[lo];
     const bool g = k >= own_tiles * o_chunks[lo];
     if (g) k -= own_tiles * o_chunks[lo];
     const int n = g ? gopens[lo] * rep : own_rows;
-    const int tiles = (n + tile.rows - 1) / tile.rows;
-    const int c = k / tiles, r0 = (k - c * tiles) * tile.rows;
+    const int tr = tile_rows(tile, MX, n), tiles = ceil_div(n, tr);
+    const int c = k / tiles, r0 = (k - c * tiles) * tr;
     const int from = g ? 0 : shares[lo];
     const int keys = g ? shares[lo] : tile_keys(ends[lo], opens[lo], from, r0, rep, tile.unit);
     const int step = even_step(g ? shares[lo] : o_len[lo], g ? g_chunks[lo] : o_chunks[lo],
@@ -288,7 +289,7 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
     Item it;
     it.q0 = qoffs[lo];
     it.r0 = r0;
-    it.nr = min(tile.rows, n - r0);
+    it.nr = min(tr, n - r0);
     it.seq = lo;
     it.k0 = from + c * step;
     it.k1 = from + min(keys, (c + 1) * step);   // not above k0: the tile has no such chunk

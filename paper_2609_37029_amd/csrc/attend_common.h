@@ -43,6 +43,12 @@ __host__ __device__ constexpr Tile tile_of(bool bf16) {
   return bf16 ? Tile{256, 4 * kStage, 256, 384} : Tile{32, 128, 512, 192};
 }
 __host__ __device__ inline Tile tile_of(const PagesShape& s) { return tile_of(s.dtype != LDR_F32); }
+// Rows of the tiles of a segment of R rows. Of a coded cache 65 to 96 rows are two tiles, of 64
+// rows and of the rest: together 15.7 us for 1024 keys (all compute units at it, 4 bits,
+// head_dim 128), as one 17.3.
+__host__ __device__ inline int tile_rows(const Tile& t, bool mx, int R) {
+  return mx && R > 64 && R <= 96 ? 64 : t.rows;
+}
 // Rounds of items over those workgroups, at most (4 took 2% longer: the
 // grid is sized for as many, and most of it ends at once).
 constexpr int kMaxRounds = 2;
@@ -90,8 +96,9 @@ AttendWs plan_ws(const PagesShape& s, int hq, int max_new) {
   const int rep = hq / s.hkv, tile = tile_of(s).rows;
   const long rows = (long)s.batch * max_new * rep;
   // every tile of the own and of the shared segments once, and the added ones
-  w.max_items = (int)((long)s.batch * (((long)max_new * rep + tile - 1) / tile) + rows / tile +
-                      s.batch / 2 + added_items(s));
+  const long tiles = ((long)max_new * rep + tile - 1) / tile;
+  w.max_items = (int)(s.batch * tiles + rows / tile + s.batch / 2 + added_items(s));
+  if (s.bits) w.max_items += s.batch + s.batch / 2;   // a second tile of 65 to 96 rows
   w.tiles = (int)(((long)max_new * rep + kBlock - 1) / kBlock);
   w.blocks = (long)s.batch * w.tiles + rows / kBlock + s.batch / 2 +
              (long)(tile / kBlock) * added_items(s);
@@ -282,7 +289,7 @@ __device__ inline void join_parts(const AttendArgs& a, const Item& it, const Seq
   // parts: the group's chunks, then the tile's own. Of few rows there are columns
   // to spare: R a part, and 32 / R parts at a time (4 rows of 32 parts, as 64
   // sequences with one token each have, took 8 loads behind one another, 11 us).
-  const int t = it.r0 / tile_of(a.s).rows * tile_of(a.s).rows;
+  const int tr = tile_rows(tile_of(a.s), a.s.bits, f.open * a.rep), t = it.r0 / tr * tr;
   const int own = f.own_chunks ? ceil_div(tile_keys(f.rows, f.open, f.share, t, a.rep,
                                                     tile_of(a.s).unit), f.step) : 0;
   const int parts = f.grp_chunks + own;

@@ -333,19 +333,18 @@ attend_mx_last_kernel(AttendArgs a) {
   it.q0 = f.qoff;
   const int cbase = f.rows - f.open;
   const Tile tile = tile_of(a.s);
-  const int t = it.r0 / tile.rows * tile.rows;
+  const int tr = tile_rows(tile, true, f.open * a.rep), t = it.r0 / tr * tr;
   it.k0 = f.share + (f.own_chunks ? tile_keys(f.rows, f.open, f.share, t, a.rep, tile.unit) : 0);
   it.k1 = cbase + (it.r0 + it.nr - 1) / a.rep + 1;
   mx_rows<BITS, D, true, W>(a, it, f, cbase, head, (int)threadIdx.x, lds);
 }
 
-// An item of 33 to 128 rows: as mx_rows, but a wave has two tiles of 32 rows (one, where
-// the second pair has no other), so that a key is decoded once or twice for all of them. The
-// waves are split between the pairs of tiles by their work; the queries are in LDS. Rows of
-// a step are loaded where those of the last one have been taken: the two waves of a SIMD
-// have the time of the other one's instructions too.
+// An item of 33 to 64 rows: as mx_rows, but a wave has both tiles of 32 rows, so that a key
+// is decoded once for them. The queries are in LDS. Rows of a step are loaded where those of
+// the last one have been taken: the two waves of a SIMD have the time of the other one's
+// instructions too.
 template <int BITS, int D>
-__device__ inline void mx_mid(const AttendArgs& a, const Item& it, int head, int tid, float* lds) {
+__device__ inline void mx_pair(const AttendArgs& a, const Item& it, int head, int tid, float* lds) {
   using Raw = RawStep<BITS, D>;
   using Page = MxPage<BITS, D>;
   constexpr int NF = D / 16, ND = D / 32, W = kWideThreads / 64, NT = kWideThreads;
@@ -357,14 +356,10 @@ __device__ inline void mx_mid(const AttendArgs& a, const Item& it, int head, int
   const uint8_t* kpool = a.p.pool + (size_t)2 * a.layer * a.s.n_pages * a.s.page_bytes +
                          head * a.s.head_bytes;
   const size_t vplane = (size_t)a.s.n_pages * a.s.page_bytes;
-  const int tiles = (it.nr + kBlock - 1) / kBlock;
-  // waves of the first pair of tiles: 5 to 3 is as 2 tiles to 1, with the decoding
-  const int w0 = tiles == 2 ? W : tiles == 3 ? 5 : 4;
-  const bool second = wave >= w0;
-  const int turn_ = second ? wave - w0 : wave, turns = second ? W - w0 : w0;
+  constexpr int N = 2;                    // tiles
 
   u32x4* qs = reinterpret_cast<u32x4*>(lds);
-  for (int f = wave; f < tiles * NF; f += W) {
+  for (int f = wave; f < N * NF; f += W) {
     const int r = it.r0 + min(f / NF * kBlock + col, it.nr - 1), qi = r / a.rep;
     const uint16_t* qp = static_cast<const uint16_t*>(a.q) +
                          (size_t)map[it.q0 + qi] * a.q_stride +
@@ -378,7 +373,7 @@ __device__ inline void mx_mid(const AttendArgs& a, const Item& it, int head, int
   const int steps = (it.k1 - it.k0) / kStep;
   const int shift = 31 - __builtin_clz(a.s.page);
   auto id_of = [&](int t) {
-    return scalar_word(table, (it.k0 + min(t * turns + turn_, steps - 1) * kStep) >> shift);
+    return scalar_word(table, (it.k0 + min(t * W + wave, steps - 1) * kStep) >> shift);
   };
   Raw x;
   int id = id_of(0);
@@ -386,7 +381,7 @@ __device__ inline void mx_mid(const AttendArgs& a, const Item& it, int head, int
   int in = 0;
   auto go_to = [&](int t) {
     page = kpool + (size_t)clamp_page(a.s, id) * a.s.page_bytes;
-    in = (it.k0 + min(t * turns + turn_, steps - 1) * kStep) & (a.s.page - 1);
+    in = (it.k0 + min(t * W + wave, steps - 1) * kStep) & (a.s.page - 1);
     id = id_of(t + 1);
   };
   auto load_k = [&]() {
@@ -407,20 +402,16 @@ __device__ inline void mx_mid(const AttendArgs& a, const Item& it, int head, int
       x.vs[p] = *reinterpret_cast<const u32x4*>(vp.vscale(2 * p + (col >> 4), in + half * 16));
     }
   };
-  // of 8-bit codes V's rows are loaded behind K's products, not before them: with both
-  // there the accumulators leave no room
-  constexpr bool kLateV = BITS == 8;
   go_to(0);
   load_k();
-  if (!kLateV) load_v();
   __syncthreads();
-  const u32x4* qw = qs + (second ? 2 * NF * 64 : 0) + lane;
-  auto run = [&](auto count) {
-    constexpr int N = decltype(count)::value;       // tiles of the wave
-    for (int t = 0; t * turns + turn_ < steps; ++t) {
+  const u32x4* qw = qs + lane;
+  {
+    for (int t = 0; t * W + wave < steps; ++t) {
+      __builtin_amdgcn_s_setprio(1);      // before the other wave's vector instructions
       f32x16 sc[N] = {};
       // query fragments kAhead products in front; held there, or all of them are in registers
-      constexpr int kAhead = 2, R = kAhead + N;
+      constexpr int kAhead = BITS == 4 ? 6 : 4, R = kAhead + N;
       u32x4 fr[R];
       auto read = [&](int n) { fr[n % R] = qw[(n % N * NF + n / N) * 64]; };
 #pragma unroll
@@ -444,7 +435,10 @@ __device__ inline void mx_mid(const AttendArgs& a, const Item& it, int head, int
           sc[u] = M16::run(u32x4{k[0], k[1], k[2], k[3]}, fr[(i * N + u) % R], sc[u]);
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (kLateV) load_v();
+      __builtin_amdgcn_s_setprio(0);
+      // V's rows of this step, not before K's products: with both there the accumulators
+      // leave no room for the queries on their way from LDS
+      load_v();
       go_to(t + 1);
       load_k();
       u32x4 pf[N][2];
@@ -474,32 +468,45 @@ __device__ inline void mx_mid(const AttendArgs& a, const Item& it, int head, int
 #pragma unroll
         for (int i = 0; i < 2; ++i) pf[u][i] = M16::pack(e + i * 8);
       }
+      // the values, eight keys of two tiles of O^T at a time: the next ones are decoded
+      // between the products
+      constexpr int G = 2 * Raw::NP;
+      u32x4 vf[2][2];
+      auto decode = [&](int g) {
+        uint32_t w[BITS / 2], even[4], odd[4];
+        const int p = g / 2, i = g % 2;
 #pragma unroll
-      for (int p = 0; p < Raw::NP; ++p)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          __builtin_amdgcn_sched_barrier(0);
-          uint32_t w[BITS / 2], even[4], odd[4];
-#pragma unroll
-          for (int j = 0; j < BITS / 2; ++j) {
-            const int at = i * (BITS / 2) + j;
-            w[j] = x.v[p][at / 4][at % 4];
-          }
-          mx_turned8<BITS>(w, x.vs[p][2 * i], x.vs[p][2 * i + 1], even, odd);
-#pragma unroll
-          for (int u = 0; u < N; ++u) {
-            o[u][2 * p] = M16::run(u32x4{even[0], even[1], even[2], even[3]}, pf[u][i], o[u][2 * p]);
-            o[u][2 * p + 1] =
-                M16::run(u32x4{odd[0], odd[1], odd[2], odd[3]}, pf[u][i], o[u][2 * p + 1]);
-          }
+        for (int j = 0; j < BITS / 2; ++j) {
+          const int at = i * (BITS / 2) + j;
+          w[j] = x.v[p][at / 4][at % 4];
         }
-      if (!kLateV) load_v();
-    }
-  };
-  if (second && tiles == 3) run(std::integral_constant<int, 1>{});
-  else run(std::integral_constant<int, 2>{});
+        mx_turned8<BITS>(w, x.vs[p][2 * i], x.vs[p][2 * i + 1], even, odd);
+        vf[g % 2][0] = u32x4{even[0], even[1], even[2], even[3]};
+        vf[g % 2][1] = u32x4{odd[0], odd[1], odd[2], odd[3]};
+      };
+      __builtin_amdgcn_sched_barrier(0);
+      decode(0);
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (g + 1 < G) decode(g + 1);
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int u = 0; u < N; ++u)
+            o[u][g / 2 * 2 + q] = M16::run(vf[g % 2][q], pf[u][g % 2], o[u][g / 2 * 2 + q]);
+        if (g + 1 < G)
+#pragma unroll
+          for (int q = 0; q < 2 * N; ++q) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);             // a product
+            __builtin_amdgcn_sched_group_barrier(0x2, 24 / (2 * N), 0);  // and decoding
+          }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+        }
+  }
 
-  // join the waves of a pair, one of its tiles after the other
+  // join the waves, a tile after the other
   constexpr int LD = D + 4;
   float* sm = lds + W * 32 * LD;
   float* sl = sm + W * 32;
@@ -509,9 +516,9 @@ __device__ inline void mx_mid(const AttendArgs& a, const Item& it, int head, int
     __syncthreads();       // the queries, or the last tile, have been read
     if (half == 0) { sm[wave * 32 + col] = mu[u]; sl[wave * 32 + col] = lu; }
     __syncthreads();
-    const int first = second ? w0 : 0;
-    float mt = -INFINITY;
-    for (int k = 0; k < turns; ++k) mt = fmaxf(mt, sm[(first + k) * 32 + col]);
+    float mt = sm[col];
+#pragma unroll
+    for (int k = 1; k < W; ++k) mt = fmaxf(mt, sm[k * 32 + col]);
     const float own = __builtin_amdgcn_exp2f(mu[u] - (mt == -INFINITY ? 0.f : mt));
     float* so = lds + (wave * 32 + col) * LD;
 #pragma unroll
@@ -522,68 +529,39 @@ __device__ inline void mx_mid(const AttendArgs& a, const Item& it, int head, int
             float4{o[u][dt][4 * g] * own, o[u][dt][4 * g + 1] * own, o[u][dt][4 * g + 2] * own,
                    o[u][dt][4 * g + 3] * own};
     __syncthreads();
-    for (int s = 0; s < 2 && 2 * s + u < tiles; ++s) {
-      const int lo = s ? w0 : 0, hi = s ? W : w0;
-      constexpr int NI = 32 * (D / 4) / NT;
+    constexpr int NI = 32 * (D / 4) / NT;
 #pragma unroll
-      for (int v = 0; v < NI; ++v) {
-        const int i = v * NT + tid, row = i % 32, e = i / 32 * 4;
-        float mm = -INFINITY, ll = 0.f;
-        float4 acc{};
-        for (int k = lo; k < hi; ++k) mm = fmaxf(mm, sm[k * 32 + row]);
-        const float mz = mm == -INFINITY ? 0.f : mm;
-        for (int k = lo; k < hi; ++k) {
-          ll += sl[k * 32 + row] * __builtin_amdgcn_exp2f(sm[k * 32 + row] - mz);
-          const float4 y = *reinterpret_cast<const float4*>(lds + (k * 32 + row) * LD + e);
-          acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
-        }
-        const long at = it.part + 2 * s + u;
-        reinterpret_cast<float4*>(part_o<D>(a, head, at))[(e / 8) * 64 + (e / 4 % 2) * 32 + row] = acc;
-        if (e == 0)
-          part_ml(a, head, at)[row] = float2{mm == -INFINITY ? mm : mm / c2, ll};
+    for (int v = 0; v < NI; ++v) {
+      const int i = v * NT + tid, row = i % 32, e = i / 32 * 4;
+      float mm = sm[row], ll = 0.f;
+      float4 acc{};
+#pragma unroll
+      for (int k = 1; k < W; ++k) mm = fmaxf(mm, sm[k * 32 + row]);
+      const float mz = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        ll += sl[k * 32 + row] * __builtin_amdgcn_exp2f(sm[k * 32 + row] - mz);
+        const float4 y = *reinterpret_cast<const float4*>(lds + (k * 32 + row) * LD + e);
+        acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
       }
+      const long at = it.part + u;
+      reinterpret_cast<float4*>(part_o<D>(a, head, at))[(e / 8) * 64 + (e / 4 % 2) * 32 + row] = acc;
+      if (e == 0) part_ml(a, head, at)[row] = float2{mm == -INFINITY ? mm : mm / c2, ll};
     }
   }
 }
 
-// The coded rows on their way to an item of many rows: a ring of stages in LDS, filled by
-// DMA. A wave loads what its own threads decode, so that it waits for its own loads and for
-// no barrier. Of a stage it has 8 K rows and 8 pairs of V's dimensions, 16 bytes a lane, in
-// one instruction where that is room enough, and their scales, 4 bytes a lane; lanes to
-// spare load something twice.
-template <int BITS, int D> struct MxRing {
-  static constexpr int N = BITS == 4 ? 8 : 4;        // stages: 8 (4 bits) or 15 KB each
-  static constexpr int KL = D * BITS / 16, VL = 8 * BITS;      // lanes of K and of V
-  static constexpr bool kOne = KL + VL <= 64;
-  static constexpr int kLoads = kOne ? 2 : 3;        // instructions of a stage
-  static constexpr int kV = kOne ? KL * 16 : 1024, kScales = kOne ? 1024 : 2048;
-  static constexpr int kWave = kScales + 256;        // bytes of a wave's stage
-  static constexpr int kBytes = N * kWave * (kWideThreads / 64);
-};
-
-// DMA of 16 (or 4) bytes a lane from its address to LDS, lane after lane from `to` on. In
-// assembly, as the compiler would wait for it at the next read of LDS, whatever that reads;
-// whoever reads what it brings waits first (wait_loads). M0 is nobody else's here.
-__device__ inline void dma16(uint32_t to, const uint8_t* from) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from)
-               : "memory");
-}
-__device__ inline void dma4(uint32_t to, const uint8_t* from) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from)
-               : "memory");
-}
-// All but the last N loads are there.
-template <int N> __device__ inline void wait_loads() {
-  static_assert(N >= 0 && N < 64, "vmcnt");
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-
-// An item of more than 128 rows: 32 a wave, over stages of 64 keys that the workgroup
-// decodes into LDS. As in the bf16 kernel the two waves of a SIMD belong to two groups half
-// a stage apart, one in the matrix unit while the other makes probabilities, and a stage has
-// one barrier. Buffer j mod 2 has K of stage j and V of j - 1, which the products of stage j
-// read between barriers j and j + 1; in the same interval every wave decodes its share of
-// the next buffer, K of j + 1 and V of j, from the ring and starts to load a later one.
+// An item of more than 64 rows: 32 a wave, over stages of 64 keys that the workgroup decodes
+// into LDS. As in the bf16 kernel the two waves of a SIMD belong to two groups half a stage
+// apart, one in the matrix unit while the other makes probabilities, and a stage has one
+// barrier. Buffer j mod 2 has K of stage j and V of j - 1, which the products of stage j read
+// between barriers j and j + 1; in the same interval every wave decodes its share of the next
+// buffer, K of j + 1 and V of j, from registers and loads what is two stages on.
+// Measured and left out: a ring of coded stages in LDS, filled by DMA (memory is not what is
+// waited for: with all keys in cache 68 rows take as long), stages of 128 keys for up to 128
+// rows, and those rows as pairs of tiles, each with waves of its own, in registers (16 sequences
+// with 60 to 68 rows over 8192 keys 70 to 77 us a layer whichever it is; of 8 bits, one with
+// 68 rows over 65536 keys 46 us so, 57 in registers).
 template <int BITS, int D, bool SMALL>
 __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, int tid, uint8_t* lds) {
   using Page = MxPage<BITS, D>;
@@ -591,8 +569,7 @@ __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, in
   constexpr int KC = D / 8;                          // 16-byte chunks of a K row in LDS
   constexpr int STAGE = kStage * D * 2;              // bytes of a stage of K (or V) there
   constexpr int KE = D / 64;                         // chunks of K that a thread decodes
-  constexpr int KB = KE * BITS / 4, VB = BITS / 2;   // words of K and V that it takes
-  using Ring = MxRing<BITS, D>;
+  constexpr int KB = KE * BITS / 4, VB = BITS / 2;   // words of K and V that it loads
   const int32_t* map = reinterpret_cast<const int32_t*>(a.ws + a.w.map);
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -602,11 +579,14 @@ __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, in
                          head * a.s.head_bytes;
   const size_t vplane = (size_t)a.s.n_pages * a.s.page_bytes;
 
-  // the lane's query; columns behind the last row repeat it
-  const bool active = wave * kBlock < it.nr;
+  // up to 128 rows: both groups take the same rows, each 32 of a stage's keys, and join
+  // at the end. The lane's query; columns behind the last row repeat it.
+  const bool split = it.nr <= NW / 2 * kBlock;
+  const int block = split ? wave % (NW / 2) : wave;
+  const bool active = block * kBlock < it.nr;
   u32x4 qf[NF];
   {
-    const int r = it.r0 + min(wave * kBlock + col, it.nr - 1), qi = r / a.rep;
+    const int r = it.r0 + min(block * kBlock + col, it.nr - 1), qi = r / a.rep;
     const uint16_t* qp = static_cast<const uint16_t*>(a.q) +
                          (size_t)map[it.q0 + qi] * a.q_stride + (head * a.rep + r - qi * a.rep) * D;
 #pragma unroll
@@ -633,42 +613,10 @@ __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, in
     p.in = SMALL ? 0 : (it.k0 + j * kStage) & (a.s.page - 1);
     return p;
   };
-  // what the lane loads: a K row's or a pair's 16 bytes, and 4 bytes of scales
-  uint8_t* const ring = lds + 4 * STAGE + wave * Ring::kWave;
-  const uint32_t ring0 = __builtin_amdgcn_readfirstlane(
-      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)ring);
-  constexpr int KLR = Page::kRow / 16, VLR = 4 * Page::kUnit;      // lanes of a row, of a pair
-  const int lk = wave * 8 + lane % Ring::KL / KLR;                 // its K row, pair, keys
-  const int lv_lane = (Ring::kOne ? lane - Ring::KL : lane) & (Ring::VL - 1);
-  const int lv = (wave * 8 + lv_lane / VLR) % (D / 2);
-  const int lv_key = lv_lane % VLR * (16 / Page::kUnit);
-  const bool is_k = lane < Ring::KL;
-  constexpr int SL = 8 * Page::kBlocks / 4;                        // lanes of K's scales
-  const bool is_ks = lane < SL;
-  const int ls = is_ks ? lane : (lane - SL) & 15;
-  const int sv_key = ls * 4, sv_block = wave * 8 % (D / 2) / (kMxBlock / 2);
-  auto start = [&](int slot, const Place& kp, const Place& vp) {
-    const uint32_t to = ring0 + slot * (Ring::kWave * NW);
-    const Page pk{SMALL && wave >= 4 ? kp.b : kp.a, a.s.page};
-    const int row = kp.in + (SMALL ? lk & 31 : lk);
-    const uint8_t* fk = pk.k(row) + lane % KLR * 16;
-    const Page pv{(SMALL && lv_key >= 32 ? vp.b : vp.a) + vplane, a.s.page};
-    const uint8_t* fv = pv.v(lv, vp.in + (SMALL ? lv_key & 31 : lv_key));
-    if constexpr (Ring::kOne) {
-      dma16(to, is_k ? fk : fv);
-    } else {
-      dma16(to, fk);
-      dma16(to + 1024, fv);
-    }
-    const int row0 = kp.in + (SMALL ? wave * 8 & 31 : wave * 8);
-    const Page ps{(SMALL && sv_key >= 32 ? vp.b : vp.a) + vplane, a.s.page};
-    dma4(to + Ring::kScales,
-         is_ks ? pk.kscale(row0) + ls * 4
-               : ps.vscale(sv_block, vp.in + (SMALL ? sv_key & 31 : sv_key)));
-  };
-  auto take = [&](auto& to, const uint8_t* from, auto n) {
+  struct Raw { uint32_t k[KB], v[VB], ks; uint2 vs; };
+  auto load = [&](auto& to, const uint32_t* from, auto n) {
     constexpr int N = decltype(n)::value;
-    if constexpr (N == 1) to[0] = *reinterpret_cast<const uint32_t*>(from);
+    if constexpr (N == 1) to[0] = from[0];
     else if constexpr (N == 2) {
       const uint2 t = *reinterpret_cast<const uint2*>(from);
       to[0] = t.x; to[1] = t.y;
@@ -677,55 +625,54 @@ __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, in
       to[0] = t[0]; to[1] = t[1]; to[2] = t[2]; to[3] = t[3];
     }
   };
-  const int ks_at = Ring::kScales + lane / 8 * Page::kBlocks + kc * KE * 8 / kMxBlock;
-  auto put_k = [&](uint8_t* to, int slot) {
-    const uint8_t* from = ring + slot * (Ring::kWave * NW);
-    uint32_t w[KB], o[4];
-    take(w, from + lane * (KB * 4), std::integral_constant<int, KB>{});
-    const float scale = mx_scale<0>(from[ks_at]);
-#pragma unroll
-    for (int c = 0; c < KE; ++c) {
-      mx_eight<BITS>(w + c * (BITS / 4), scale, o);
-      *reinterpret_cast<u32x4*>(to + kr * (2 * D) + (((kc * KE + c) ^ turn<KC>(kr)) << 4)) =
-          u32x4{o[0], o[1], o[2], o[3]};
-    }
+  auto load_k = [&](Raw& x, const Place& p) {
+    const Page pg{SMALL && wave >= 4 ? p.b : p.a, a.s.page};
+    const int row = p.in + (SMALL ? kr & 31 : kr);
+    load(x.k, reinterpret_cast<const uint32_t*>(pg.k(row) + kc * (KB * 4)),
+         std::integral_constant<int, KB>{});
+    x.ks = pg.kscale(row)[kc * KE * 8 / kMxBlock];
+  };
+  auto load_v = [&](Raw& x, const Place& p) {
+    if (!has_v) return;
+    const Page pg{(SMALL && oct >= 4 ? p.b : p.a) + vplane, a.s.page};
+    const int row = p.in + (SMALL ? oct % 4 : oct) * 8;
+    load(x.v, reinterpret_cast<const uint32_t*>(pg.v(vp, row)), std::integral_constant<int, VB>{});
+    x.vs = *reinterpret_cast<const uint2*>(pg.vscale(vp / (kMxBlock / 2), row));
+  };
+  auto put_k = [&](uint8_t* to, const Raw& x, int c) {     // chunk c of the thread's
+    uint32_t o[4];
+    mx_eight<BITS>(x.k + c * (BITS / 4), mx_scale<0>(x.ks), o);
+    *reinterpret_cast<u32x4*>(to + kr * (2 * D) + (((kc * KE + c) ^ turn<KC>(kr)) << 4)) =
+        u32x4{o[0], o[1], o[2], o[3]};
   };
   const int vrow = (vp >> 5) * 64 + (vp & 31);             // of the even dimension in LDS
-  auto put_v = [&](uint8_t* to, int slot) {
+  auto put_v = [&](uint8_t* to, const Raw& x) {
     if (!has_v) return;
-    const uint8_t* from = ring + slot * (Ring::kWave * NW);
-    uint32_t w[VB], even[4], odd[4];
-    take(w, from + Ring::kV + lane * (VB * 4), std::integral_constant<int, VB>{});
-    const uint2 sc = *reinterpret_cast<const uint2*>(from + Ring::kScales + SL * 4 + oct * 8);
-    mx_turned8<BITS>(w, sc.x, sc.y, even, odd);
+    uint32_t even[4], odd[4];
+    mx_turned8<BITS>(x.v, x.vs.x, x.vs.y, even, odd);
     uint8_t* at = to + vrow * 128 + ((oct ^ turn<8>(vrow)) << 4);   // 32 rows on, the same
     *reinterpret_cast<u32x4*>(at) = u32x4{even[0], even[1], even[2], even[3]};
     *reinterpret_cast<u32x4*>(at + 32 * 128) = u32x4{odd[0], odd[1], odd[2], odd[3]};
   };
 
-  // slot j mod N of the ring: K of stage j and V of j - 1
+  // the set of stage j + 1 (its K, and V of j) is ra or rb by j + 1's parity
+  Raw ra, rb;
   Ids next;       // pages of the next K to load
-  Place kp, vpl;  // where the K and V of the next slot to load are
-  auto advance = [&](int j) {    // to the slot of stage j
+  Place kp, vpl;  // where the K and V of the next set to load are
+  auto advance = [&](int j) {    // to the set of stage j
     vpl = kp;
     kp = place(next, min(j, stages - 1));
     next = ids_of(min(j + 1, stages - 1));
   };
-  constexpr int kTasks = 3;
-  // task q of stage j, J = j mod 4: K and V of the next buffer, and the loads N stages on,
-  // into the slot that they leave
-  auto task = [&](auto J, int j, int q) {
-    uint8_t* to = lds + ((decltype(J)::value + 1) & 1) * 2 * STAGE;
-    const int slot = (j + 1) & (Ring::N - 1);
-    if (q == 0) {
-      wait_loads<(Ring::N - 1) * Ring::kLoads>();
-      put_k(to, slot);
-    } else if (q == 1) {
-      put_v(to + STAGE, slot);
-    } else {
-      advance(j + 1 + Ring::N);
-      start(slot, kp, vpl);
-    }
+  constexpr int kTasks = KE + 2;
+  // task q of stage j, its parity odd or not: of the next buffer's decoding, and the loads
+  auto task = [&](auto Odd, int j, int q) {
+    constexpr bool ODD = decltype(Odd)::value;
+    uint8_t* to = lds + (ODD ? 0 : 2 * STAGE);
+    Raw& x = ODD ? ra : rb;
+    if (q < KE) put_k(to, x, q);
+    else if (q == KE) put_v(to + STAGE, x);
+    else { advance(j + 3); load_k(x, kp); load_v(x, vpl); }
   };
 
   // fragments: K rows in the order that leaves a lane 8 consecutive keys. The
@@ -740,30 +687,31 @@ __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, in
   float mu = -INFINITY, l = 0.f;
   f32x16 sc[2];
   u32x4 pf[4] = {};      // none before the first stage, and its V is 0
-  // The products of stage j, J = j mod 4: V^T P^T of j - 1, then (unless j is the end) K Q^T
-  // of j, two at a time, with the LDS reads kAhead fragments in front of them and the tasks
-  // between them.
-  auto products = [&](auto scores, auto J, int j) {
+  // The products of stage j: V^T P^T of j - 1, then (unless j is the end) K Q^T of j, two
+  // at a time, with the LDS reads kAhead fragments in front of them and the tasks between
+  // them. Half: 0 or 1, or both (2).
+  auto products = [&](auto scores, auto Half, auto Odd, int j) {
+    constexpr int H = decltype(Half)::value, NS = H == 2 ? 2 : 1, F0 = H == 1 ? 2 : 0;
     constexpr int G = 2, kAhead = 4, R = kAhead + G;
-    constexpr int NV = 4 * ND, N = NV + (decltype(scores)::value ? 2 * NF : 0);
+    constexpr int NV = 2 * NS * ND, N = NV + (decltype(scores)::value ? NS * NF : 0);
     constexpr int EACH = N / kTasks < G ? G : N / kTasks / G * G;     // products a task
     static_assert(N % G == 0 && kAhead % G == 0, "whole groups");
     static_assert(!decltype(scores)::value || EACH * kTasks <= N, "room for every task");
-    const uint8_t* kb = lds + (decltype(J)::value & 1) * 2 * STAGE;
-    const uint8_t* vb = kb + STAGE;
+    const uint8_t* kb = lds + (decltype(Odd)::value ? 2 * STAGE : 0) + (H == 1 ? 64 * D : 0);
+    const uint8_t* vb = lds + (decltype(Odd)::value ? 3 * STAGE : STAGE);
     u32x4 fr[R];
     auto read = [&](int i) {
-      const int f = i < NV ? i / ND : (i - NV) / 2;
+      const int f = i < NV ? F0 + i / ND : (i - NV) / NS;
       fr[i % R] = i < NV ? *reinterpret_cast<const u32x4*>(vb + (vlane ^ (f << 5)) + i % ND * 4096)
                          : *reinterpret_cast<const u32x4*>(kb + (klane ^ (f << 5)) +
-                                                           (i - NV) % 2 * (64 * D));
+                                                           (i - NV) % NS * (64 * D));
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) read(i);
 #pragma unroll
     for (int i0 = 0; i0 < N; i0 += G) {
       __builtin_amdgcn_sched_barrier(0x6);
-      if (decltype(scores)::value && i0 % EACH == 0 && i0 / EACH < kTasks) task(J, j, i0 / EACH);
+      if (decltype(scores)::value && i0 % EACH == 0 && i0 / EACH < kTasks) task(Odd, j, i0 / EACH);
 #pragma unroll
       for (int i = i0 + kAhead; i < i0 + kAhead + G; ++i)
         if (i < N) read(i);
@@ -773,17 +721,19 @@ __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, in
         if (i < NV) {
           o[i % ND] = M16::run(fr[i % R], pf[i / ND], o[i % ND]);
         } else {
-          const int f = (i - NV) / 2, sub = (i - NV) % 2;
+          const int f = (i - NV) / NS, sub = (i - NV) % NS;
           sc[sub] = M16::run(fr[i % R], qf[f], f ? sc[sub] : f32x16{});
         }
       }
     }
     __builtin_amdgcn_sched_barrier(0x6);
   };
-  auto softmax = [&]() {
-    float mx = fmaxf(sc[0][0], sc[1][0]);
+  auto softmax = [&](auto Half) {
+    constexpr int NS = decltype(Half)::value == 2 ? 2 : 1;
+    float mx = sc[0][0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, fmaxf(sc[0][i], sc[1][i]));
+    for (int i = NS == 2 ? 0 : 1; i < 16; ++i)
+      mx = fmaxf(mx, NS == 2 ? fmaxf(sc[0][i], sc[1][i]) : sc[0][i]);
     mx = half_max(mx) * c2;
     const bool up = mx > mu + kLazy;
     if (__any(up)) {
@@ -797,7 +747,7 @@ __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, in
     const float z = mu == -INFINITY ? 0.f : mu;
     float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
+    for (int sub = 0; sub < NS; ++sub) {
       float x[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -815,73 +765,100 @@ __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, in
   std::integral_constant<int, 0> i0;
   std::integral_constant<int, 1> i1;
   std::integral_constant<int, 2> i2;
-  std::integral_constant<int, 3> i3;
   // what is in LDS is there before the barrier; loads in flight go on
   auto meet = [&]() {
     __builtin_amdgcn_sched_barrier(0);
     lds_barrier();
     __builtin_amdgcn_sched_barrier(0);
   };
-  // buffer 0: K of stage 0, no V yet; the slots of stages 1 to N
+  // buffer 0: K of stage 0, no V yet; the sets of stages 1 and 2
   {
     kp = place(ids_of(0), 0);
     next = ids_of(min(1, stages - 1));
-    start(0, kp, kp);
-    for (int j = 1; j < Ring::N; ++j) {
-      advance(j);
-      start(j, kp, vpl);
-    }
+    load_k(ra, kp);
     u32x4* zero = reinterpret_cast<u32x4*>(lds + STAGE);
     for (int i = tid; i < STAGE / 16; i += kWideThreads) zero[i] = u32x4{};
-    wait_loads<(Ring::N - 1) * Ring::kLoads>();
-    put_k(lds, 0);
-    advance(Ring::N);
-    start(0, kp, vpl);
+    advance(1);
+    load_k(rb, kp);
+    load_v(rb, vpl);
+#pragma unroll
+    for (int c = 0; c < KE; ++c) put_k(lds, ra, c);
+    advance(2);
+    load_k(ra, kp);
+    load_v(ra, vpl);
   }
   // the stages of a wave without rows (its share of the decoding, and the barriers),
   // of the first group, or of the second
-  auto run = [&](auto works, auto late) {
+  auto run = [&](auto works, auto late, auto Half) {
     constexpr bool WORKS = decltype(works)::value, LATE = decltype(late)::value;
-    auto stage = [&](auto J, int j) {
+    auto stage = [&](auto Odd, int j) {
       if constexpr (!LATE) meet();
       if constexpr (WORKS) {
         __builtin_amdgcn_s_setprio(1);
-        products(yes, J, j);
+        products(yes, Half, Odd, j);
         __builtin_amdgcn_s_setprio(0);
       } else {
 #pragma unroll
-        for (int q = 0; q < kTasks; ++q) task(J, j, q);
+        for (int q = 0; q < kTasks; ++q) task(Odd, j, q);
       }
       if constexpr (LATE) meet();
-      if constexpr (WORKS) softmax();
+      if constexpr (WORKS) softmax(Half);
     };
     if constexpr (LATE) meet();
-    for (int j = 0; j < stages; j += 4) {   // whole fours
-      stage(i0, j);
-      stage(i1, j + 1);
-      stage(i2, j + 2);
-      stage(i3, j + 3);
+    for (int j = 0; j < stages; j += 2) {   // whole twos
+      stage(no, j);
+      stage(yes, j + 1);
     }
     if constexpr (!LATE) meet();            // as many barriers as the other group's
-    if constexpr (WORKS) products(no, i0, stages);
+    if constexpr (WORKS) products(no, Half, no, stages);
   };
-  if (!active) run(no, no);
-  else if (wave < NW / 2) run(yes, no);
-  else run(yes, yes);
-  wait_loads<0>();   // no DMA outlives the workgroup
+  if (!active) run(no, no, i2);
+  else if (wave < NW / 2) { if (split) run(yes, no, i0); else run(yes, no, i2); }
+  else { if (split) run(yes, yes, i1); else run(yes, yes, i2); }
   l = half_sum(l);
 
+  if (split) {       // the second group's results reach the first through LDS
+    __syncthreads();
+    float4* po = reinterpret_cast<float4*>(lds + block * STAGE) + lane;
+    float2* ml = reinterpret_cast<float2*>(lds + 4 * STAGE) + block * kBlock;
+    if (wave >= NW / 2) {
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          po[(dt * 4 + g) * 64] = float4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2],
+                                         o[dt][4 * g + 3]};
+      if (half == 0) ml[col] = float2{mu, l};
+    }
+    __syncthreads();
+    if (wave >= NW / 2 || !active) return;      // from the item
+    const float2 x = ml[col];
+    const float mn = fmaxf(mu, x.x), z = mn == -INFINITY ? 0.f : mn;
+    const float wo = __builtin_amdgcn_exp2f(mu - z), wx = __builtin_amdgcn_exp2f(x.x - z);
+    mu = mn;
+    l = l * wo + x.y * wx;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 v = po[(dt * 4 + g) * 64];
+        o[dt][4 * g] = o[dt][4 * g] * wo + v.x * wx;
+        o[dt][4 * g + 1] = o[dt][4 * g + 1] * wo + v.y * wx;
+        o[dt][4 * g + 2] = o[dt][4 * g + 2] * wo + v.z * wx;
+        o[dt][4 * g + 3] = o[dt][4 * g + 3] * wo + v.w * wx;
+      }
+  }
   if (!active) return;      // from the item
 
   // the wave's block of partial results, straight from the registers
-  float4* out = reinterpret_cast<float4*>(part_o<D>(a, head, it.part + wave)) + lane;
+  float4* out = reinterpret_cast<float4*>(part_o<D>(a, head, it.part + block)) + lane;
 #pragma unroll
   for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
     for (int g = 0; g < 4; ++g)
       out[(dt * 4 + g) * 64] = float4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2],
                                       o[dt][4 * g + 3]};
-  if (half == 0) part_ml(a, head, it.part + wave)[col] = float2{mu / c2, l};
+  if (half == 0) part_ml(a, head, it.part + block)[col] = float2{mu / c2, l};
 }
 
 // SMALL: pages of 32 rows, half a stage.
@@ -890,7 +867,7 @@ __global__ void __launch_bounds__(kWideThreads) __attribute__((amdgpu_waves_per_
 attend_mx_kernel(AttendArgs a) {
   constexpr int W = kWideThreads / 64;
   constexpr int kRows = (W * 32 * (D + 4) + 68 * W) * 4;
-  constexpr int kWide = 4 * kStage * D * 2 + MxRing<BITS, D>::kBytes;
+  constexpr int kWide = 4 * kStage * D * 2 + W / 2 * kBlock * 8;
   __shared__ alignas(1024) uint8_t lds[kRows > kWide ? kRows : kWide];
   const int items = scalar_word(a.ws, 3);
   if (!plan_ok(a, items)) return;
@@ -905,8 +882,8 @@ attend_mx_kernel(AttendArgs a) {
     asm volatile("" : "+v"(tid));
     if (it.nr <= kBlock)
       mx_rows<BITS, D, false, W>(a, it, SeqInfo{}, 0, head, tid, reinterpret_cast<float*>(lds));
-    else if (it.nr <= 4 * kBlock)
-      mx_mid<BITS, D>(a, it, head, tid, reinterpret_cast<float*>(lds));
+    else if (it.nr <= 2 * kBlock)
+      mx_pair<BITS, D>(a, it, head, tid, reinterpret_cast<float*>(lds));
     else
       mx_wide<BITS, D, SMALL>(a, it, head, tid, lds);
     __syncthreads();

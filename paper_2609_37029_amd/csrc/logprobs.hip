@@ -11,7 +11,7 @@
 // The n largest entries are among the n groups of 64 neighbours with the largest maxima (in
 // the order by value, then by index: a group that is not has n entries before any of its
 // own). The first pass writes the maxima; the second picks the groups, then the entries in
-// them, with sorted lists of 64 keys across the lanes of a wave.
+// them (select).
 //
 // Bound by the one read of the logits.
 #include "ldr_internal.h"
@@ -44,15 +44,25 @@ struct LogprobsArgs {
 // Larger entries have larger keys; a NaN's is the lowest.
 __device__ inline uint32_t key_of(float z) { return z == z ? order_key(z) : 0u; }
 
-__device__ inline float wave_max(float v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
-  return v;
+// Over a wave, in every lane: rows of 16 by lane swaps, then the four rows.
+__device__ inline float lane_of(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
 }
-template <typename T> __device__ inline T wave_sum(T v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
-  return v;
+__device__ inline float wave_max(float v) {
+  v = max16(v);
+  return fmaxf(fmaxf(lane_of(v, 0), lane_of(v, 16)), fmaxf(lane_of(v, 32), lane_of(v, 48)));
+}
+__device__ inline float wave_sum(float v) {
+  v = sum16(v);
+  return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
+__device__ inline int wave_sum(int v) {
+  v += __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, false);
+  v += __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, false);
+  v += __builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, false);
+  v += __builtin_amdgcn_mov_dpp(v, 0x140, 0xF, 0xF, false);
+  return __builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16) +
+         __builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48);
 }
 
 // One piece of 1024 U entries: thread t has four of every 1024.
@@ -139,66 +149,130 @@ __global__ void __launch_bounds__(kThreads) logprobs_pieces_kernel(LogprobsArgs 
   }
 }
 
-// Keys across a wave, the largest in lane 0.
-struct Key { uint32_t hi, lo; };     // the value's key, the index's complement
-__device__ inline bool ahead(const Key& a, const Key& b) {
-  return a.hi > b.hi || (a.hi == b.hi && a.lo > b.lo);
+// An entry's place in the order: its value's key above the complement of its index, so that
+// no two are equal; 0: none.
+typedef uint64_t Key;
+__device__ inline Key place_of(uint32_t key, int index) { return (Key)key << 32 | (uint32_t)~index; }
+__device__ inline int index_of(Key k) { return (int)~(uint32_t)k; }
+
+template <int CTRL> __device__ inline Key key_dpp(Key k) {
+  const uint32_t lo = __builtin_amdgcn_mov_dpp((int)(uint32_t)k, CTRL, 0xF, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_mov_dpp((int)(uint32_t)(k >> 32), CTRL, 0xF, 0xF, false);
+  return (Key)hi << 32 | lo;
 }
-__device__ inline Key from_lane(const Key& k, int mask) {
-  return Key{(uint32_t)__shfl_xor((int)k.hi, mask), (uint32_t)__shfl_xor((int)k.lo, mask)};
+__device__ inline Key key_lane(Key k, int lane) {
+  return (Key)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(k >> 32), lane) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, lane);
+}
+// The largest of a wave, in every lane.
+__device__ inline Key wave_max(Key k) {
+  k = max(k, key_dpp<0xB1>(k));     // quads
+  k = max(k, key_dpp<0x4E>(k));
+  k = max(k, key_dpp<0x141>(k));    // half rows, rows of 16
+  k = max(k, key_dpp<0x140>(k));
+  return max(max(key_lane(k, 0), key_lane(k, 16)), max(key_lane(k, 32), key_lane(k, 48)));
+}
+__device__ inline Key key_xor(Key k, int mask) {
+  return (Key)(uint32_t)__shfl_xor((int)(uint32_t)(k >> 32), mask) << 32 |
+         (uint32_t)__shfl_xor((int)(uint32_t)k, mask);
 }
 // The larger (or the smaller) of a lane's key and that of the lane `mask` away.
 __device__ inline void exchange(Key& k, int mask, bool larger) {
-  const Key o = from_lane(k, mask);
-  if (ahead(o, k) == larger) k = o;
+  const Key o = key_xor(k, mask);
+  if ((o > k) == larger) k = o;
 }
-__device__ inline void sort64(Key& k) {
+// The 64 largest of a wave's sorted list (lane 0 first) and of 64 keys more.
+__device__ inline void add64(Key& list, Key k, bool sorted) {
   const int lane = threadIdx.x & 63;
+  if (!sorted) {
 #pragma unroll
-  for (int size = 2; size <= 64; size <<= 1)
+    for (int size = 2; size <= 64; size <<= 1)
 #pragma unroll
-    for (int off = size >> 1; off >= 1; off >>= 1)
-      exchange(k, off, ((lane & off) == 0) == ((lane & size) == 0));
-}
-// The 64 largest of two sorted lists, `o` turned round (lane l has its entry 63 - l).
-__device__ inline void merge64(Key& k, const Key& o) {
-  const int lane = threadIdx.x & 63;
-  if (ahead(o, k)) k = o;
+      for (int off = size >> 1; off >= 1; off >>= 1)
+        exchange(k, off, ((lane & off) == 0) == ((lane & size) == 0));
+  }
+  list = max(list, key_xor(k, 63));
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) exchange(k, off, (lane & off) == 0);
+  for (int off = 32; off >= 1; off >>= 1) exchange(list, off, (lane & off) == 0);
 }
-// Up to 64 more keys into a wave's list, of which the first n count.
-__device__ inline void add64(Key& list, Key k, int n) {
-  const Key last{(uint32_t)__shfl((int)list.hi, n - 1), (uint32_t)__shfl((int)list.lo, n - 1)};
-  if (!__any(ahead(k, last))) return;
-  sort64(k);
-  merge64(list, from_lane(k, 63));
-}
-// The waves' lists into one that all of them have; `lds`: 64 a wave.
-__device__ inline void join_lists(Key& list, Key* lds, int lane, int wave) {
+
+constexpr int kMost = kWaves * 64;      // candidates that are ranked by counting
+struct SelectLds { Key keys[kMost], least[kWaves], picked[kMostTop]; int count; };
+
+// The n largest of `m` keys, in order, to lds.picked (0 behind them); get(i): key i. Each
+// wave's k-th largest of its threads' maxima, k kWaves >= n, leaves n keys at or above the
+// least of them; keys above that are few, unless one wave has nothing but small ones, and
+// each counts those before it. Neighbours belong to different waves, so that keys in order
+// do not do that. Where there are too many, the waves keep sorted lists and join them (20
+// of a row's 2374 maxima and of their groups: 15 us so, 5 by counting).
+template <typename F>
+__device__ inline void select(SelectLds& lds, int n, int m, F get) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int first = lane * kWaves + wave;
+  Key best = 0;
+  for (int i = first; i < m; i += kMost) best = max(best, get(i));
+  Key kth = 0;
+  for (int k = 0; k < n; k += kWaves) {
+    kth = wave_max(best);
+    if (best == kth) best = 0;
+  }
+  if (lane == 0) lds.least[wave] = kth;
+  if (tid == 0) lds.count = 0;
+  if (tid < kMostTop) lds.picked[tid] = 0;
   __syncthreads();
-  lds[wave * 64 + lane] = list;
+  Key least = lds.least[0];
 #pragma unroll
-  for (int n = kWaves / 2; n >= 1; n >>= 1) {
-    __syncthreads();
-    if (wave < n) {
-      merge64(list, lds[(wave + n) * 64 + 63 - lane]);
-      lds[wave * 64 + lane] = list;
-    }
+  for (int w = 1; w < kWaves; ++w) least = min(least, lds.least[w]);
+  for (int i0 = 0; i0 < m; i0 += kMost) {
+    const int i = i0 + first;
+    const Key k = i < m ? get(i) : 0;
+    const uint64_t in = __ballot(k != 0 && k >= least);
+    if (in == 0) continue;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&lds.count, __builtin_popcountll(in));
+    at = __builtin_amdgcn_readfirstlane(at) + __builtin_popcountll(in & ((1ull << lane) - 1));
+    if (in >> lane & 1 && at < kMost) lds.keys[at] = k;
   }
   __syncthreads();
-  list = lds[lane];
+  const int count = lds.count;
+  if (count <= kMost) {
+    if (tid < count) {
+      const Key mine = lds.keys[tid];
+      int rank = 0;
+#pragma unroll 8
+      for (int j = 0; j < count; ++j) rank += lds.keys[j] > mine;
+      if (rank < n) lds.picked[rank] = mine;
+    }
+    __syncthreads();
+    return;
+  }
+  Key list = 0;
+  for (int i0 = 0; i0 < m; i0 += kMost) {
+    const int i = i0 + first;
+    const Key k = i < m ? get(i) : 0;
+    if (__any(k > key_lane(list, n - 1))) add64(list, k, false);
+  }
+  lds.keys[tid] = list;
+#pragma unroll
+  for (int w = kWaves / 2; w >= 1; w >>= 1) {
+    __syncthreads();
+    if (wave < w) {
+      add64(list, lds.keys[tid + w * 64], true);
+      lds.keys[tid] = list;
+    }
+  }
+  if (tid < n) lds.picked[tid] = list;
+  __syncthreads();
 }
 
 // The pieces of a row, and what is left of each row's answer.
 template <bool TOP>
 __global__ void __launch_bounds__(TOP ? kWaves * 64 : 64) logprobs_rows_kernel(LogprobsArgs a) {
-  __shared__ Key lists[TOP ? kWaves * 64 : 1];
   const int b = blockIdx.y, i = blockIdx.x;
   if (a.n_rows && i >= a.n_rows[b]) return;
   const size_t row = (size_t)b * a.rows + i;
   const float* z = a.z + row * a.stride;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
   const Piece* parts = a.parts + row * a.pieces;
   const int y = a.tokens[row];
   const bool given = y >= 0 && y < a.vocab;
@@ -234,26 +308,21 @@ __global__ void __launch_bounds__(TOP ? kWaves * 64 : 64) logprobs_rows_kernel(L
     a.rank[row] = given ? before : a.vocab;
   }
   if constexpr (TOP) {
-    // groups, then the entries of the first `top` of them
-    Key list{0u, 0u};
+    __shared__ SelectLds lds;
+    __shared__ int groups[kMostTop];
     const uint32_t* maxima = a.maxima + row * a.groups;
-    for (int g0 = wave * 64; g0 < a.groups; g0 += kWaves * 64) {
-      const int g = g0 + lane;
-      add64(list, g < a.groups ? Key{maxima[g], ~(uint32_t)g} : Key{0u, 0u}, a.top);
-    }
-    join_lists(list, lists, lane, wave);
-    Key best{0u, 0u};
+    select(lds, a.top, a.groups, [&](int g) { return place_of(maxima[g], g); });
     const int n = min(a.top, a.groups);
-    for (int j = wave; j < n; j += kWaves) {
-      const uint32_t g = ~(uint32_t)__shfl((int)list.lo, j);
-      const int v = (int)g * kGroup + lane;
-      add64(best, v < a.vocab ? Key{key_of(z[v]), ~(uint32_t)v} : Key{0u, 0u}, a.top);
-    }
-    join_lists(best, lists, lane, wave);
-    if (wave == 0 && lane < a.top) {
-      const int v = (int)~best.lo;
-      a.top_tokens[row * a.top + lane] = v;
-      a.top_logp[row * a.top + lane] = logp(z[v]);
+    if (threadIdx.x < n) groups[threadIdx.x] = index_of(lds.picked[threadIdx.x]);
+    __syncthreads();
+    select(lds, a.top, n * kGroup, [&](int i) {
+      const int v = groups[i / kGroup] * kGroup + i % kGroup;
+      return v < a.vocab ? place_of(key_of(z[v]), v) : 0;
+    });
+    if (threadIdx.x < a.top) {
+      const int v = index_of(lds.picked[threadIdx.x]);
+      a.top_tokens[row * a.top + threadIdx.x] = v;
+      a.top_logp[row * a.top + threadIdx.x] = logp(z[v]);
     }
   }
 }

@@ -113,6 +113,19 @@ def test_the_largest_entries_close_together_or_apart(gpu_lib):
     _check(gpu_lib, z, [[650, 128, 0, 0, V - 1]], 64)
 
 
+def test_one_wave_with_nothing_but_small_entries(gpu_lib):
+    """Every sixteenth group, or every sixteenth entry, far below the others: no threshold
+    leaves few candidates."""
+    V = 151936
+    z = _z((1, 3, V), 61, 1.0)
+    at = torch.arange(V, device="cuda")
+    z[0, 0] -= 100.0 * (at // 64 % 16 == 3)
+    z[0, 1] -= 100.0 * (at % 16 == 15)
+    z[0, 2] = torch.where((at // 64 % 16 == 0) | (at % 16 == 0), -50.0, 1.0)
+    _check(gpu_lib, z, [[5, 6, 7]], 64)
+    _check(gpu_lib, z, [[5, 6, 7]], 17)
+
+
 def test_masked_entries(gpu_lib):
     """-inf: entries without probability; rows with one entry left, and with none."""
     z = _z((1, 6, 4100), 7)
