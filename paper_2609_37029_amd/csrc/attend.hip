@@ -382,7 +382,66 @@ attend_rows_kernel(AttendArgs a) {
   };
   if (wave < steps) fetch(0);
   if constexpr (FINISH) {
-    join_parts<D, W>(a, it, f, head, wave, c2, o, m, l);
+    // parts: the group's chunks, then the tile's own. Of few rows there are columns
+    // to spare: R a part, and 32 / R parts at a time (4 rows of 32 parts, as 64
+    // sequences with one token each have, took 8 loads behind one another, 11 us).
+    const int t = it.r0 / tile_of(a.s).rows * tile_of(a.s).rows;
+    const int own = f.own_chunks
+                        ? (tile_keys(f.rows, f.open, f.share, t, a.rep, tile_of(a.s).unit) + f.step - 1) / f.step : 0;
+    const int parts = f.grp_chunks + own;
+    int R = 32;
+    while (R > 1 && 2 * it.nr <= R && W * 32 < parts * R) R >>= 1;
+    const int rp = it.r0 + min(col & (R - 1), it.nr - 1), gr = f.grp_off + rp;
+    for (int c = wave + W * (col / R); c < parts; c += W * (32 / R)) {
+      const bool g = c < f.grp_chunks;
+      const long block = g ? f.grp_part + (long)c * f.grp_blocks + gr / kBlock
+                           : f.own_part + (long)(c - f.grp_chunks) * f.own_blocks + it.r0 / kBlock;
+      const int at = g ? gr % kBlock : rp % kBlock;
+      const float2 ml = part_ml(a, head, block)[at];
+      const float4* po = reinterpret_cast<const float4*>(part_o<D>(a, head, block)) + half * 32 + at;
+      float4 v[D / 8];
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) v[i] = po[i * 64];
+      const float mn = fmaxf(m, ml.x), mu = mn == -INFINITY ? 0.f : mn;
+      const float wo = __builtin_amdgcn_exp2f((m - mu) * c2);
+      const float wp = __builtin_amdgcn_exp2f((ml.x - mu) * c2);
+      m = mn;
+      l = l * wo + ml.y * wp;
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) {
+        const int dt = i / 4, q = i % 4 * 4;
+        o[dt][q] = o[dt][q] * wo + v[i].x * wp;
+        o[dt][q + 1] = o[dt][q + 1] * wo + v[i].y * wp;
+        o[dt][q + 2] = o[dt][q + 2] * wo + v[i].z * wp;
+        o[dt][q + 3] = o[dt][q + 3] * wo + v[i].w * wp;
+      }
+    }
+    if (R < 32) {            // the columns of a row, to their common maximum and added up
+      float mn = fmaxf(m, aside<16>(m));
+      if (R < 16) mn = fmaxf(mn, aside<8>(mn));
+      if (R < 8) mn = fmaxf(mn, aside<4>(mn));
+      if (R < 4) mn = fmaxf(mn, aside<2>(mn));
+      if (R < 2) mn = fmaxf(mn, aside<1>(mn));
+      const float w = __builtin_amdgcn_exp2f((m - (mn == -INFINITY ? 0.f : mn)) * c2);
+      m = mn;
+      l *= w;
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) o[dt] *= w;
+      auto add = [&](auto off) {
+        constexpr int OFF = decltype(off)::value;
+        l += aside<OFF>(l);
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[dt][i] += aside<OFF>(o[dt][i]);
+      };
+      add(std::integral_constant<int, 16>{});
+      if (R < 16) add(std::integral_constant<int, 8>{});
+      if (R < 8) add(std::integral_constant<int, 4>{});
+      if (R < 4) add(std::integral_constant<int, 2>{});
+      if (R < 2) add(std::integral_constant<int, 1>{});
+    }
+    l = half ? 0.f : l;      // of both halves; the steps' sums are of one each
   }
   for (int t = 0; t * W + wave < steps; ++t) {
     const int kb = it.k0 + (t * W + wave) * kStep;
