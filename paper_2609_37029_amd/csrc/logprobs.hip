@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kGroup = 64;        // neighbours that share a maximum
-constexpr int kWaves = 16;        // of a workgroup that picks entries
+constexpr int kPicked = 4096;     // keys that a workgroup which picks entries holds
 constexpr int kMostTop = 64;
 
 // An exponent whose power is 0: -inf times that is to be 0 too.
@@ -196,81 +196,107 @@ __device__ inline void add64(Key& list, Key k, bool sorted) {
   for (int off = 32; off >= 1; off >>= 1) exchange(list, off, (lane & off) == 0);
 }
 
-constexpr int kMost = kWaves * 64;      // candidates that are ranked by counting
-struct SelectLds { Key keys[kMost], least[kWaves], picked[kMostTop]; int count; };
+template <int W> struct SelectLds { Key keys[W * 64], least[W], picked[kMostTop]; int count; };
 
-// The n largest of `m` keys, in order, to lds.picked (0 behind them); get(i): key i. Each
-// wave's k-th largest of its threads' maxima, k kWaves >= n, leaves n keys at or above the
-// least of them; keys above that are few, unless one wave has nothing but small ones, and
-// each counts those before it. Neighbours belong to different waves, so that keys in order
-// do not do that. Where there are too many, the waves keep sorted lists and join them (20
-// of a row's 2374 maxima and of their groups: 15 us so, 5 by counting).
-template <typename F>
-__device__ inline void select(SelectLds& lds, int n, int m, F get) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int first = lane * kWaves + wave;
-  Key best = 0;
-  for (int i = first; i < m; i += kMost) best = max(best, get(i));
-  Key kth = 0;
-  for (int k = 0; k < n; k += kWaves) {
-    kth = wave_max(best);
-    if (best == kth) best = 0;
-  }
-  if (lane == 0) lds.least[wave] = kth;
-  if (tid == 0) lds.count = 0;
-  if (tid < kMostTop) lds.picked[tid] = 0;
-  __syncthreads();
-  Key least = lds.least[0];
+// A workgroup's W waves take the n largest of `m` keys, in order, to lds.picked (0 behind
+// them); get(i): key i. Each wave's k-th largest of its threads' maxima, k W >= n, leaves n
+// keys at or above the least of them; keys above that are few, unless one wave has nothing
+// but small ones, and each counts those before it. Neighbours belong to different waves, so
+// that keys in order do not do that. Where there are too many, the waves keep sorted lists and
+// join them (20 of a row's 2374 maxima, then of their groups: 15 us so, 8 by counting).
+template <int W, typename F> struct Select {
+  static constexpr int NT = W * 64, R = kPicked / NT;
+  SelectLds<W>& lds;
+  int n, m;
+  F get;
+  Key held[R];       // the first kPicked keys, R a thread; those behind them are taken again
+
+  __device__ static int first() { return (threadIdx.x & 63) * W + (threadIdx.x >> 6); }
+  __device__ Select(SelectLds<W>& l, int n, int m, F f) : lds(l), n(n), m(m), get(f) {
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) least = min(least, lds.least[w]);
-  for (int i0 = 0; i0 < m; i0 += kMost) {
-    const int i = i0 + first;
-    const Key k = i < m ? get(i) : 0;
-    const uint64_t in = __ballot(k != 0 && k >= least);
-    if (in == 0) continue;
-    int at = 0;
-    if (lane == 0) at = atomicAdd(&lds.count, __builtin_popcountll(in));
-    at = __builtin_amdgcn_readfirstlane(at) + __builtin_popcountll(in & ((1ull << lane) - 1));
-    if (in >> lane & 1 && at < kMost) lds.keys[at] = k;
+    for (int t = 0; t < R; ++t) held[t] = t * NT + first() < m ? get(t * NT + first()) : 0;
   }
-  __syncthreads();
-  const int count = lds.count;
-  if (count <= kMost) {
-    if (tid < count) {
-      const Key mine = lds.keys[tid];
-      int rank = 0;
+  // f(key) for the thread's keys, all threads at once
+  template <typename G> __device__ void each(G f) {
+#pragma unroll
+    for (int t = 0; t < R; ++t)
+      if (t * NT < m) f(held[t]);
+    for (int i0 = kPicked; i0 < m; i0 += NT) f(i0 + first() < m ? get(i0 + first()) : 0);
+  }
+  __device__ void run() {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    Key best = 0;
+    each([&](Key k) { best = max(best, k); });
+    Key kth = 0;
+    for (int k = 0; k < n; k += W) {
+      kth = wave_max(best);
+      if (best == kth) best = 0;
+    }
+    if (lane == 0) lds.least[wave] = kth;
+    if (tid == 0) lds.count = 0;
+    if (tid < kMostTop) lds.picked[tid] = 0;
+    __syncthreads();
+    Key least = lds.least[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) least = min(least, lds.least[w]);
+    each([&](Key k) {
+      const uint64_t in = __ballot(k != 0 && k >= least);
+      if (in == 0) return;
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&lds.count, __builtin_popcountll(in));
+      at = __builtin_amdgcn_readfirstlane(at) + __builtin_popcountll(in & ((1ull << lane) - 1));
+      if (in >> lane & 1 && at < NT) lds.keys[at] = k;
+    });
+    __syncthreads();
+    const int count = lds.count;
+    if (count <= NT) {
+      if (tid < count) {
+        const Key mine = lds.keys[tid];
+        int rank = 0;
 #pragma unroll 8
-      for (int j = 0; j < count; ++j) rank += lds.keys[j] > mine;
-      if (rank < n) lds.picked[rank] = mine;
+        for (int j = 0; j < count; ++j) rank += lds.keys[j] > mine;
+        if (rank < n) lds.picked[rank] = mine;
+      }
+      __syncthreads();
+      return;
     }
-    __syncthreads();
-    return;
-  }
-  Key list = 0;
-  for (int i0 = 0; i0 < m; i0 += kMost) {
-    const int i = i0 + first;
-    const Key k = i < m ? get(i) : 0;
-    if (__any(k > key_lane(list, n - 1))) add64(list, k, false);
-  }
-  lds.keys[tid] = list;
+    Key list = 0;
+    each([&](Key k) {
+      if (__any(k > key_lane(list, n - 1))) add64(list, k, false);
+    });
+    lds.keys[tid] = list;
 #pragma unroll
-  for (int w = kWaves / 2; w >= 1; w >>= 1) {
-    __syncthreads();
-    if (wave < w) {
-      add64(list, lds.keys[tid + w * 64], true);
-      lds.keys[tid] = list;
+    for (int w = W / 2; w >= 1; w >>= 1) {
+      __syncthreads();
+      if (wave < w) {
+        add64(list, lds.keys[tid + w * 64], true);
+        lds.keys[tid] = list;
+      }
     }
+    if (tid < n) lds.picked[tid] = list;
+    __syncthreads();
   }
-  if (tid < n) lds.picked[tid] = list;
-  __syncthreads();
+};
+template <int W, typename F>
+__device__ inline Select<W, F> select(SelectLds<W>& lds, int n, int m, F f) {
+  return Select<W, F>(lds, n, m, f);
 }
 
-// The pieces of a row, and what is left of each row's answer.
-template <bool TOP>
-__global__ void __launch_bounds__(TOP ? kWaves * 64 : 64) logprobs_rows_kernel(LogprobsArgs a) {
+// The pieces of a row, and what is left of each row's answer, by W waves; W = 1: without the
+// largest entries. With them: 8 waves (one row of 151936, 20 entries, both launches: 13.3 us;
+// 16.7 with 16, 14.3 with 4), or 4 where there are many rows (1024 rows, the largest entry of
+// each, this launch: 42 us with 16 and 14 with 4).
+template <int W>
+__global__ void __launch_bounds__(W * 64) logprobs_rows_kernel(LogprobsArgs a) {
+  constexpr bool TOP = W > 1;
   const int b = blockIdx.y, i = blockIdx.x;
   if (a.n_rows && i >= a.n_rows[b]) return;
   const size_t row = (size_t)b * a.rows + i;
+  __shared__ SelectLds<W> lds;
+  __shared__ int groups[kMostTop];
+  const uint32_t* maxima = a.maxima + row * a.groups;
+  // on their way while the pieces are joined
+  auto by_group = select(lds, a.top, TOP ? a.groups : 0, [&](int g) { return place_of(maxima[g], g); });
   const float* z = a.z + row * a.stride;
   const int lane = threadIdx.x & 63;
   const Piece* parts = a.parts + row * a.pieces;
@@ -308,17 +334,14 @@ __global__ void __launch_bounds__(TOP ? kWaves * 64 : 64) logprobs_rows_kernel(L
     a.rank[row] = given ? before : a.vocab;
   }
   if constexpr (TOP) {
-    __shared__ SelectLds lds;
-    __shared__ int groups[kMostTop];
-    const uint32_t* maxima = a.maxima + row * a.groups;
-    select(lds, a.top, a.groups, [&](int g) { return place_of(maxima[g], g); });
+    by_group.run();
     const int n = min(a.top, a.groups);
     if (threadIdx.x < n) groups[threadIdx.x] = index_of(lds.picked[threadIdx.x]);
     __syncthreads();
     select(lds, a.top, n * kGroup, [&](int i) {
       const int v = groups[i / kGroup] * kGroup + i % kGroup;
       return v < a.vocab ? place_of(key_of(z[v]), v) : 0;
-    });
+    }).run();
     if (threadIdx.x < a.top) {
       const int v = index_of(lds.picked[threadIdx.x]);
       a.top_tokens[row * a.top + threadIdx.x] = v;
@@ -366,10 +389,13 @@ hipError_t launch_logprobs(const float* logits, int64_t stride, const int32_t* t
   else launch_pieces<2>(a, batch, st);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (top)
-    hipLaunchKernelGGL(logprobs_rows_kernel<true>, dim3(rows, batch), dim3(kWaves * 64), 0, st, a);
+  const dim3 grid(rows, batch);
+  if (top == 0)
+    hipLaunchKernelGGL(logprobs_rows_kernel<1>, grid, dim3(64), 0, st, a);
+  else if (n <= 512)
+    hipLaunchKernelGGL(logprobs_rows_kernel<8>, grid, dim3(512), 0, st, a);
   else
-    hipLaunchKernelGGL(logprobs_rows_kernel<false>, dim3(rows, batch), dim3(64), 0, st, a);
+    hipLaunchKernelGGL(logprobs_rows_kernel<4>, grid, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -93,6 +93,24 @@ def test_many_rows_take_larger_pieces(gpu_lib):
     _check(gpu_lib, z, y, 20)
 
 
+@pytest.mark.parametrize("top", [1, 20, 64])
+def test_many_rows_are_picked_by_fewer_waves(gpu_lib, top):
+    """More than 512 rows; vocabularies whose maxima are more than a workgroup holds."""
+    z = _z((3, 171, 700), top)
+    z[0, :50] = torch.round(z[0, :50])
+    z[1, 7, ::2] = -float("inf")
+    z[1, 8] = float("nan")
+    _check(gpu_lib, z, np.random.default_rng(top).integers(0, 700, (3, 171)), top)
+
+
+def test_large_vocabularies(gpu_lib):
+    V = 4096 * 64 + 700
+    z = _z((1, 2, V), 31)
+    z[0, 1] -= 40.0 * (torch.arange(V, device="cuda") // 64 % 16 == 5)
+    z[0, 1, -3:] += 60.0
+    _check(gpu_lib, z, [[V - 1, 4]], 64)
+
+
 def test_ties_go_to_the_lowest_index(gpu_lib):
     z = torch.zeros(1, 4, 5000, device="cuda")
     z[0, 1, ::7] = 1.0
@@ -114,16 +132,27 @@ def test_the_largest_entries_close_together_or_apart(gpu_lib):
 
 
 def test_one_wave_with_nothing_but_small_entries(gpu_lib):
-    """Every sixteenth group, or every sixteenth entry, far below the others: no threshold
+    """Every fourth (eighth, sixteenth) group, or entry, far below the others: no threshold
     leaves few candidates."""
     V = 151936
-    z = _z((1, 3, V), 61, 1.0)
     at = torch.arange(V, device="cuda")
-    z[0, 0] -= 100.0 * (at // 64 % 16 == 3)
-    z[0, 1] -= 100.0 * (at % 16 == 15)
-    z[0, 2] = torch.where((at // 64 % 16 == 0) | (at % 16 == 0), -50.0, 1.0)
-    _check(gpu_lib, z, [[5, 6, 7]], 64)
-    _check(gpu_lib, z, [[5, 6, 7]], 17)
+    for w in (4, 8, 16):
+        z = _z((1, 3, V), 61, 1.0)
+        z[0, 0] -= 100.0 * (at // 64 % w == 3)
+        z[0, 1] -= 100.0 * (at % w == w - 1)
+        z[0, 2] = torch.where((at // 64 % w == 0) | (at % w == 0), -50.0, 1.0)
+        _check(gpu_lib, z, [[5, 6, 7]], 64)
+        _check(gpu_lib, z, [[5, 6, 7]], 17)
+
+
+def test_one_wave_of_four_with_nothing_but_small_entries(gpu_lib):
+    """The same where many rows are picked by four waves."""
+    V = 20000
+    at = torch.arange(V, device="cuda")
+    z = _z((2, 300, V), 62, 1.0)
+    z[0] -= 100.0 * (at // 64 % 4 == 3)
+    z[1] -= 100.0 * (at % 4 == 1)
+    _check(gpu_lib, z, np.zeros((2, 300), int), 30)
 
 
 def test_masked_entries(gpu_lib):
