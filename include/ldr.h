@@ -354,7 +354,7 @@ int ldr_pages_write(ldr_pages* p, int32_t layer, int32_t n_layers, const void* K
  * outside [0, max_rows], is left out whole and sets the sticky LDR_ERANGE flag.
  *   first, n  dev int32 [batch]
  *   K, V      dev [batch][max_rows][n_layers][n_kv_heads][head_dim], of the rows'
- *             type, 16-byte aligned */
+ *             type, 16-byte aligned, not over each other (LDR_EINVAL) */
 int ldr_pages_read(const ldr_pages* p, int32_t layer, int32_t n_layers, const int32_t* first,
                    const int32_t* n, void* K, void* V, int32_t max_rows, void* stream);
 
@@ -420,7 +420,8 @@ int ldr_attend_plan(const ldr_pages* p, int32_t n_q_heads, int32_t max_new,
  * -inf still multiplies its v by 0. What masked places hold does not count,
  * infinities and NaN included. Rows i >= open[b] of o and lse stay as they were.
  * n_q_heads and max_new are the plan's.
- * A coded cache is attended to as a bf16 cache of the values that its codes stand for.
+ * A coded cache is attended to as a bf16 cache of the values that its codes stand for
+ * (its last kernel keeps 16 bits of the probabilities).
  *   q    dev dtype (bf16 for a coded cache), row (b, i) at q + (b max_new + i) q_stride elements, its
  *        [n_q_heads][head_dim] contiguous; q_stride a multiple of 8 (bf16) or 4
  *   o    dev [batch][max_new][n_q_heads][head_dim] dtype; may be q, if q is laid

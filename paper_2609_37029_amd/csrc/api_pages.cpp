@@ -128,6 +128,9 @@ int ldr_pages_read(const ldr_pages* p, int32_t layer, int32_t n_layers, const in
   if (!first || !n || !aligned(first, 4) || !aligned(n, 4)) return LDR_EINVAL;
   if (max_rows < 1 || max_rows > (1 << 28) || !K || !V || !aligned(K, 16) || !aligned(V, 16))
     return LDR_EINVAL;
+  const uintptr_t k = (uintptr_t)K, v = (uintptr_t)V;
+  if ((k < v ? v - k : k - v) < (size_t)p->s.batch * max_rows * n_layers * p->s.hkv * p->s.d * p->s.el)
+    return LDR_EINVAL;      // one over the other
   return done(launch_pages_read(p->s, p->p, layer, n_layers, first, n, K, V, max_rows,
                                 static_cast<hipStream_t>(stream)));
 }

@@ -3,17 +3,26 @@
 //
 // The decoded values are bf16 numbers, so products, sums, probabilities and their rounding
 // are those of the attention over a bf16 cache. A pair of dimensions is decoded by one
-// conversion, at the rate of an ordinary vector instruction, in the two ways that suit the
-// work:
+// conversion, at the rate of an ordinary vector instruction, in the ways that suit the work:
 //
 // Items of up to 32 rows (a token a sequence): every wave takes steps of 32 keys of its
 // own and decodes them into the operands of its products; nothing waits for another
-// wave until the end. Bound by HBM: a step's bytes take a SIMD's share of it 2140 cycles
-// (4 bits, head_dim 128), its products 512 and its vector instructions about 1300.
+// wave until the end. Bound by HBM: 16 sequences with one row over 16384 keys, 32 query and 8
+// K/V heads of 128, 4 bits, 58 us a layer (280 MB, 4.8 TB/s); with all keys in cache 48.
 //
-// More rows: the workgroup decodes a stage of 64 keys into LDS once for all of its waves,
-// in the layout, and between the products, of the bf16 kernel. Bound by the matrix unit
-// and the vector instructions of the softmax, as that one is.
+// Up to 64 rows: the same with two tiles of rows a wave.
+//
+// More: the workgroup decodes a stage of 64 keys into LDS once for all of its waves, in the
+// layout, and between the products, of the bf16 kernel. 64 sequences with one row over 32768
+// keys in common, 8 bits, 45 us a layer; 2 with 512 rows over 8192, 4 bits, 128 us (28 and
+// 108 us of a large matrix product).
+//
+// What bounds the last two: a wave's matrix products and its vector instructions (the
+// exponentials and their neighbours, 110 a tile and step of 32 keys, and 130 of decoding) take
+// turns more than they overlap: a step takes nearly the sum of both, whatever the order in
+// which they are issued, the priorities of the two waves of a SIMD, or the distance between
+// them; one wave a SIMD, with 512 registers and nothing waiting in LDS, was slower still (a
+// lone wave issues a vector instruction every 5 to 9 cycles, two one every 4.3).
 //
 // K and q may be taken along head_dim in any order that is the same for both, keys in any
 // order that is the same for P and V, and the dimensions of O in any order that all parts
@@ -50,17 +59,12 @@ template <int BITS, int D> struct MxPage {
   }
 };
 
-// One value of a page, where few are needed.
-template <int BITS> __device__ inline float nibble(const uint8_t* pair, int odd, uint8_t scale) {
-  return mx_value<BITS>(BITS == 4 ? *pair >> (4 * odd) & 15 : pair[odd], scale);
-}
-template <int BITS, int D>
-__device__ inline float value_of_k(const MxPage<BITS, D>& p, int row, int dim) {
-  return nibble<BITS>(p.k(row) + dim / 2 * (BITS / 4), dim & 1, p.kscale(row)[dim / kMxBlock]);
-}
+// One value of a V page, where few are needed.
 template <int BITS, int D>
 __device__ inline float value_of_v(const MxPage<BITS, D>& p, int row, int dim) {
-  return nibble<BITS>(p.v(dim / 2, row), dim & 1, *p.vscale(dim / kMxBlock, row));
+  const uint8_t* pair = p.v(dim / 2, row);
+  const uint32_t code = BITS == 4 ? *pair >> (4 * (dim & 1)) & 15 : pair[dim & 1];
+  return mx_value<BITS>(code, *p.vscale(dim / kMxBlock, row));
 }
 
 // Into a wave's o, m and l (column col: row it.r0 + col of sequence it.seq): the parts of

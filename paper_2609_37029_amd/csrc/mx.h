@@ -36,8 +36,9 @@ template <> struct Mx<8> {
   static constexpr int kLimitExp = 9, kLowest = -117;
 };
 
-// Scale byte B of a word, as the conversions take it: the exponent of a float, whose
-// other bits they do not look at.
+// Scale byte B of a word, as the conversions take it: the exponent of a float, whose other
+// bits they do not look at (all 256 exponents with several mantissas and signs give the same
+// value of every code, and 255 gives NaN).
 template <int B> __device__ inline float mx_scale(uint32_t w) {
   static_assert(B >= 0 && B < 4, "a byte of the word");
   return __uint_as_float(B == 3 ? w >> 1 : w << (23 - 8 * B));
@@ -61,8 +62,8 @@ template <int BITS> __device__ inline void mx_eight(const uint32_t* w, float sca
   out[3] = mx_pair<BITS, 3>(w, scale);
 }
 
-// Eight rows of a pair of dimensions (BITS / 2 ... words), their scales the bytes of two
-// words: pairs as they come, one a row.
+// Eight rows of a pair of dimensions (BITS / 2 words), their scales the bytes of two words:
+// pairs as they come, one a row.
 template <int BITS>
 __device__ inline void mx_rows8(const uint32_t* w, uint32_t s0, uint32_t s1, uint32_t* out) {
   out[0] = mx_pair<BITS, 0>(w, mx_scale<0>(s0));

@@ -4,7 +4,11 @@
 // for rows of bf16 and fp32. Tiles begin at multiples of 16 positions: V's pairs and
 // scales are stored by runs of 16 bytes along the positions, and no two workgroups write
 // to one run. Four lanes have the 32 dimensions of a block; V's codes, a quarter of its
-// rows' bytes or a half, are what goes through LDS. Bound by HBM.
+// rows' bytes or a half, are what goes through LDS.
+//
+// Bound by HBM. Measured, Qwen3-8B heads, five layers, pages of 64: 1536 rows of each of two
+// sequences into 8 bits 23 us (95 MB in and out, 4.2 TB/s) and back 20 us; 16 x 13 rows into 4
+// bits 7 us and back 5; 49000 rows of 4 bits out 285 us (1.3 GB, 4.5 TB/s).
 #include "mx.h"
 
 namespace ldr {

@@ -172,3 +172,16 @@ def test_ranges_outside_a_sequence_are_left_out(gpu_lib, held):
         assert np.array_equal(V[2, :4, 0].double().cpu().numpy(), ov[:4])
         assert c.g.status(clear=True) == gpu_lib.LDR_ERANGE
     assert c.g.status() == gpu_lib.LDR_OK
+
+
+def test_reads_over_each_other_are_refused(gpu_lib):
+    c = BothCoded(gpu_lib, 4, 1, 1, 64, 32, 8, 1, 4)
+    c.append([5])
+    both = torch.zeros(1, 9, 1, 1, 64, dtype=BF, device="cuda")
+    for K, V in ((both[:, :5], both[:, :5]), (both[:, :5], both[:, 4:]), (both[:, 4:], both[:, :5])):
+        with pytest.raises(gpu_lib.LdrError) as e:
+            c.g.read(i32([0]), i32([5]), out=(K, V))
+        assert e.value.code == gpu_lib.LDR_EINVAL
+    c.g.read(i32([0]), i32([4]), out=(both[:, :4], both[:, 4:8]))
+    torch.cuda.synchronize()
+    assert bool(both[:, :8].any()) and not both[:, 8].any()
