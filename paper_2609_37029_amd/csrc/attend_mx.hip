@@ -37,9 +37,9 @@ namespace {
 using M16 = Mma<uint16_t>;
 
 // What a lane has of a step of 32 keys, as it is in the cache: half of a K row, and 16 keys
-// of a pair of dimensions for each two tiles of O^T.
-template <int BITS, int D> struct RawStep {
-  static constexpr int KW = D * BITS / 256, VW = BITS / 4, NP = D / 64;
+// of a pair of dimensions for each two tiles of O^T (NPL of them).
+template <int BITS, int D, int NPL = D / 64> struct RawStep {
+  static constexpr int KW = D * BITS / 256, VW = BITS / 4, NP = NPL;
   u32x4 k[KW], v[NP][VW], vs[NP];
   uint32_t ks;
 };
@@ -68,11 +68,13 @@ __device__ inline float value_of_v(const MxPage<BITS, D>& p, int row, int dim) {
 }
 
 // Into a wave's o, m and l (column col: row it.r0 + col of sequence it.seq): the parts of
-// its rows, which W waves take in turn; l in the first half alone.
-template <int D, int W>
+// its rows, which W waves take in turn; l in the first half alone. Of O^T the 2 NPL tiles
+// from pair p0 of them on, U parts on their way at a time.
+template <int D, int W, int NPL, int U>
 __device__ inline void join_parts(const AttendArgs& a, const Item& it, const SeqInfo& f, int head,
-                                  int wave, float c2, f32x16 (&o)[D / 32], float& m, float& l) {
-  constexpr int ND = D / 32;
+                                  int wave, int p0, float c2, f32x16 (&o)[2 * NPL], float& m,
+                                  float& l) {
+  constexpr int ND = 2 * NPL, NV = 8 * NPL;
   const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
   // parts: the group's chunks, then the tile's own. Of few rows there are columns
   // to spare: R a part, and 32 / R parts at a time (4 rows of 32 parts, as 64
@@ -83,29 +85,39 @@ __device__ inline void join_parts(const AttendArgs& a, const Item& it, const Seq
   const int parts = f.grp_chunks + own;
   int R = 32;
   while (R > 1 && 2 * it.nr <= R && W * 32 < parts * R) R >>= 1;
-  const int rp = it.r0 + min(col & (R - 1), it.nr - 1), gr = f.grp_off + rp;
-  for (int c = wave + W * (col / R); c < parts; c += W * (32 / R)) {
-    const bool g = c < f.grp_chunks;
-    const long block = g ? f.grp_part + (long)c * f.grp_blocks + gr / kBlock
-                         : f.own_part + (long)(c - f.grp_chunks) * f.own_blocks + it.r0 / kBlock;
-    const int at = g ? gr % kBlock : rp % kBlock;
-    const float2 ml = part_ml(a, head, block)[at];
-    const float4* po = reinterpret_cast<const float4*>(part_o<D>(a, head, block)) + half * 32 + at;
-    float4 v[D / 8];
+  const int rp = it.r0 + min(col & (R - 1), it.nr - 1), gr = f.grp_off + rp, each = W * (32 / R);
+  for (int c0 = wave + W * (col / R); c0 < parts; c0 += U * each) {
+    float2 ml[U];
+    float4 v[U][NV];
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) v[i] = po[i * 64];
-    const float mn = fmaxf(m, ml.x), mu = mn == -INFINITY ? 0.f : mn;
-    const float wo = __builtin_amdgcn_exp2f((m - mu) * c2);
-    const float wp = __builtin_amdgcn_exp2f((ml.x - mu) * c2);
-    m = mn;
-    l = l * wo + ml.y * wp;
+    for (int u = 0; u < U; ++u) {
+      const int c = min(c0 + u * each, parts - 1);
+      const bool g = c < f.grp_chunks;
+      const long block = g ? f.grp_part + (long)c * f.grp_blocks + gr / kBlock
+                           : f.own_part + (long)(c - f.grp_chunks) * f.own_blocks + it.r0 / kBlock;
+      const int at = g ? gr % kBlock : rp % kBlock;
+      ml[u] = part_ml(a, head, block)[at];
+      const float4* po = reinterpret_cast<const float4*>(part_o<D>(a, head, block)) + half * 32 + at +
+                         p0 * 512;
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-      const int dt = i / 4, q = i % 4 * 4;
-      o[dt][q] = o[dt][q] * wo + v[i].x * wp;
-      o[dt][q + 1] = o[dt][q + 1] * wo + v[i].y * wp;
-      o[dt][q + 2] = o[dt][q + 2] * wo + v[i].z * wp;
-      o[dt][q + 3] = o[dt][q + 3] * wo + v[i].w * wp;
+      for (int i = 0; i < NV; ++i) v[u][i] = po[i * 64];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u && c0 + u * each >= parts) continue;
+      const float mn = fmaxf(m, ml[u].x), mu = mn == -INFINITY ? 0.f : mn;
+      const float wo = __builtin_amdgcn_exp2f((m - mu) * c2);
+      const float wp = __builtin_amdgcn_exp2f((ml[u].x - mu) * c2);
+      m = mn;
+      l = l * wo + ml[u].y * wp;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int dt = i / 4, q = i % 4 * 4;
+        o[dt][q] = o[dt][q] * wo + v[u][i].x * wp;
+        o[dt][q + 1] = o[dt][q + 1] * wo + v[u][i].y * wp;
+        o[dt][q + 2] = o[dt][q + 2] * wo + v[u][i].z * wp;
+        o[dt][q + 3] = o[dt][q + 3] * wo + v[u][i].w * wp;
+      }
     }
   }
   if (R < 32) {            // the columns of a row, to their common maximum and added up
@@ -137,14 +149,15 @@ __device__ inline void join_parts(const AttendArgs& a, const Item& it, const Seq
 }
 
 // Rows it.r0 .. + it.nr (32 at most) over the keys it.k0 .. it.k1, by W waves; `lds`: room
-// for W 32 (D + 4) + 68 W words. FINISH: also the rows' parts; the keys may end anywhere,
-// row r sees those up to cbase + r / rep, and the results are written.
-template <int BITS, int D, bool FINISH, int W>
+// for W 32 (64 NPL + 4) + 68 W words. FINISH: also the rows' parts; the keys may end anywhere,
+// row r sees those up to cbase + r / rep, and the results are written. Of O the NPL pairs of
+// tiles from p0 on: dimensions 64 p0 .. 64 (p0 + NPL) - 1.
+template <int BITS, int D, bool FINISH, int W, int NPL>
 __device__ inline void mx_rows(const AttendArgs& a, const Item& it, const SeqInfo& f, int cbase,
-                               int head, int tid, float* lds) {
-  using Raw = RawStep<BITS, D>;
+                               int head, int p0, int tid, float* lds) {
+  using Raw = RawStep<BITS, D, NPL>;
   using Page = MxPage<BITS, D>;
-  constexpr int NF = D / 16, ND = D / 32, NT = W * 64;
+  constexpr int NF = D / 16, ND = 2 * NPL, DL = 64 * NPL, NT = W * 64;
   const int32_t* map = reinterpret_cast<const int32_t*>(a.ws + a.w.map);
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -194,16 +207,17 @@ __device__ inline void mx_rows(const AttendArgs& a, const Item& it, const SeqInf
     else x.ks = kp.kscale(in + krow)[half];
 #pragma unroll
     for (int p = 0; p < Raw::NP; ++p) {
-      const u32x4* va = reinterpret_cast<const u32x4*>(vp.v(p * 32 + col, in + half * 16));
+      const u32x4* va = reinterpret_cast<const u32x4*>(vp.v((p0 + p) * 32 + col, in + half * 16));
 #pragma unroll
       for (int i = 0; i < Raw::VW; ++i) x.v[p][i] = va[i];
-      x.vs[p] = *reinterpret_cast<const u32x4*>(vp.vscale(2 * p + (col >> 4), in + half * 16));
+      x.vs[p] = *reinterpret_cast<const u32x4*>(vp.vscale(2 * (p0 + p) + (col >> 4), in + half * 16));
     }
     id = id_of(t + 1);
   };
   Raw ra, rb;
   if (wave < steps) fetch(ra, 0);
-  if constexpr (FINISH) join_parts<D, W>(a, it, f, head, wave, c2, o, m, l);
+  if constexpr (FINISH)
+    join_parts<D, W, NPL, NPL * 64 < D ? 2 : 1>(a, it, f, head, wave, p0, c2, o, m, l);
   float mu = m == -INFINITY ? -INFINITY : m * c2;
 
   auto step = [&](const Raw& now, Raw& next, int t) {
@@ -298,7 +312,7 @@ __device__ inline void mx_rows(const AttendArgs& a, const Item& it, const SeqInf
   // join the waves: each one's (m, l) of the 32 rows, then O scaled to the common
   // maximum and added up, four values a thread. O in its dimensions' order for the
   // results, as the products leave it for a part.
-  constexpr int LD = D + 4;
+  constexpr int LD = DL + 4;
   float* sm = lds + W * 32 * LD;
   float* sl = sm + W * 32;
   int* odds = reinterpret_cast<int*>(sl + W * 32);
@@ -333,9 +347,9 @@ __device__ inline void mx_rows(const AttendArgs& a, const Item& it, const SeqInf
     }
   __syncthreads();
   // thread i: values e .. e + 3 of a row; rows fastest for a part's order
-  constexpr int NI = 32 * (D / 4) / NT;
-  auto row_of = [](int i) { return FINISH ? i / (D / 4) : i % 32; };
-  auto el_of = [](int i) { return FINISH ? i % (D / 4) * 4 : i / 32 * 4; };
+  constexpr int NI = 32 * (DL / 4) / NT;
+  auto row_of = [](int i) { return FINISH ? i / (DL / 4) : i % 32; };
+  auto el_of = [](int i) { return FINISH ? i % (DL / 4) * 4 : i / 32 * 4; };
   float acc[NI][4], ll[NI], mm[NI];
 #pragma unroll
   for (int u = 0; u < NI; ++u) {
@@ -375,7 +389,7 @@ __device__ inline void mx_rows(const AttendArgs& a, const Item& it, const SeqInf
           const int in = k & (a.s.page - 1);
 #pragma unroll
           for (int d = 0; d < 4; ++d) {
-            const float v = value_of_v(vp, in, e + d);
+            const float v = value_of_v(vp, in, p0 * 64 + e + d);
             if (!(fabsf(v) < INFINITY)) acc[u][d] += v;
           }
         }
@@ -394,8 +408,8 @@ __device__ inline void mx_rows(const AttendArgs& a, const Item& it, const SeqInf
       if (row >= it.nr) continue;
       const int rr = it.r0 + row, q = rr / a.rep;
       const size_t at = ((size_t)it.seq * a.max_new + q) * a.hq + head * a.rep + (rr - q * a.rep);
-      M16::store4(static_cast<uint16_t*>(a.o) + at * D + e, acc[u]);
-      if (e == 0 && a.lse) a.lse[at] = ll[u] == 0.f ? -INFINITY : mm[u] * a.scale + logf(ll[u]);
+      M16::store4(static_cast<uint16_t*>(a.o) + at * D + p0 * 64 + e, acc[u]);
+      if (e == 0 && p0 == 0 && a.lse) a.lse[at] = ll[u] == 0.f ? -INFINITY : mm[u] * a.scale + logf(ll[u]);
     } else {
       reinterpret_cast<float4*>(part_o<D>(a, head, it.part))[(e / 8) * 64 + (e / 4 % 2) * 32 + row] =
           float4{acc[u][0], acc[u][1], acc[u][2], acc[u][3]};
@@ -406,12 +420,13 @@ __device__ inline void mx_rows(const AttendArgs& a, const Item& it, const SeqInf
 
 // The last kernel: the parts of 32 rows, the keys behind them, and the results.
 // W waves: 4, two workgroups a compute unit; 8 where no more workgroups than compute units
-// are there.
-template <int BITS, int D, int W>
+// are there. NPL: of the dimensions, all or half, two workgroups for them.
+template <int BITS, int D, int W, int NPL>
 __global__ void __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 attend_mx_last_kernel(AttendArgs a) {
-  __shared__ alignas(16) float lds[W * 32 * (D + 4) + 68 * W];
-  const int unit = (int)(blockIdx.x / a.s.hkv), head = (int)(blockIdx.x % a.s.hkv);
+  __shared__ alignas(16) float lds[W * 32 * (64 * NPL + 4) + 68 * W];
+  constexpr int SPLIT = D / 64 / NPL;
+  const int unit = (int)(blockIdx.x / SPLIT / a.s.hkv), head = (int)(blockIdx.x / SPLIT % a.s.hkv);
   const int items = scalar_word(a.ws, 3);
   Item it{};
   it.seq = unit / a.w.tiles;
@@ -425,7 +440,8 @@ attend_mx_last_kernel(AttendArgs a) {
   const int tr = tile_rows(tile, true, f.open * a.rep), t = it.r0 / tr * tr;
   it.k0 = f.share + (f.own_chunks ? tile_keys(f.rows, f.open, f.share, t, a.rep, tile.unit) : 0);
   it.k1 = cbase + (it.r0 + it.nr - 1) / a.rep + 1;
-  mx_rows<BITS, D, true, W>(a, it, f, cbase, head, (int)threadIdx.x, lds);
+  mx_rows<BITS, D, true, W, NPL>(a, it, f, cbase, head, (int)blockIdx.x % SPLIT * NPL,
+                                 (int)threadIdx.x, lds);
 }
 
 // An item of 33 to 64 rows: as mx_rows, but a wave has both tiles of 32 rows, so that a key
@@ -970,7 +986,8 @@ attend_mx_kernel(AttendArgs a) {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));
     if (it.nr <= kBlock)
-      mx_rows<BITS, D, false, W>(a, it, SeqInfo{}, 0, head, tid, reinterpret_cast<float*>(lds));
+      mx_rows<BITS, D, false, W, D / 64>(a, it, SeqInfo{}, 0, head, 0, tid,
+                                         reinterpret_cast<float*>(lds));
     else if (it.nr <= 2 * kBlock)
       mx_pair<BITS, D>(a, it, head, tid, reinterpret_cast<float*>(lds));
     else
@@ -992,10 +1009,20 @@ template <int BITS, int D> hipError_t launch(const AttendArgs& a, hipStream_t st
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t last = (int64_t)a.s.batch * a.w.tiles * a.s.hkv;
-  if (last <= kSlots)
-    hipLaunchKernelGGL((attend_mx_last_kernel<BITS, D, 8>), dim3((unsigned)last), dim3(512), 0, st, a);
+  // Few workgroups are bound by their chain of loads: two for the dimensions of 32 rows, unless
+  // one would write over queries that the other reads.
+  const char *q = static_cast<const char*>(a.q), *o = static_cast<const char*>(a.o);
+  const int64_t rows = (int64_t)a.s.batch * a.max_new;
+  const bool apart = o + rows * a.hq * D * 2 <= q || q + rows * a.q_stride * 2 <= o;
+  if (D == 128 && 2 * last <= kSlots && apart)
+    hipLaunchKernelGGL((attend_mx_last_kernel<BITS, D, 8, 1>), dim3((unsigned)last * 2), dim3(512), 0,
+                       st, a);
+  else if (last <= kSlots)
+    hipLaunchKernelGGL((attend_mx_last_kernel<BITS, D, 8, D / 64>), dim3((unsigned)last), dim3(512),
+                       0, st, a);
   else
-    hipLaunchKernelGGL((attend_mx_last_kernel<BITS, D, 4>), dim3((unsigned)last), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((attend_mx_last_kernel<BITS, D, 4, D / 64>), dim3((unsigned)last), dim3(256),
+                       0, st, a);
   return hipGetLastError();
 }
 

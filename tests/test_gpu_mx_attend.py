@@ -69,6 +69,17 @@ def test_shared_fronts(gpu_lib, bits, d, hq, hkv, page, new):
         _run(gpu_lib, c, hq, new, groups=i32(groups), q=q)
 
 
+@pytest.mark.parametrize("bits,d", [(4, 128), (8, 128), (4, 64), (8, 64)])
+@pytest.mark.parametrize("hq", [8, 64])
+def test_many_sequences(gpu_lib, bits, d, hq):
+    """More items than run at once, and more rows than one workgroup a compute unit; items
+    of one tile, of two, and of 72 rows, which are two items."""
+    c = BothCoded(gpu_lib, bits, 1, 8, d, 64, 560, 40, 14, seed=hq)
+    c.append([0, 1, 63, 600, 700] + [513 + 3 * i for i in range(35)])
+    c.append([9 - i % 3 for i in range(40)], 9)
+    _run(gpu_lib, c, hq, 9, before=2.0)
+
+
 @pytest.mark.parametrize("bits", [4, 8])
 def test_many_rows(gpu_lib, bits):
     """More query rows than a tile, the last tile of one row, many chunks."""
