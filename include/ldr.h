@@ -421,7 +421,8 @@ int ldr_attend_plan(const ldr_pages* p, int32_t n_q_heads, int32_t max_new,
  * infinities and NaN included. Rows i >= open[b] of o and lse stay as they were.
  * n_q_heads and max_new are the plan's.
  * A coded cache is attended to as a bf16 cache of the values that its codes stand for
- * (its last kernel keeps 16 bits of the probabilities).
+ * (keys near the mask and short runs of keys keep 16 bits of the probabilities, long runs
+ * the 8 of a bf16 cache).
  *   q    dev dtype (bf16 for a coded cache), row (b, i) at q + (b max_new + i) q_stride elements, its
  *        [n_q_heads][head_dim] contiguous; q_stride a multiple of 8 (bf16) or 4
  *   o    dev [batch][max_new][n_q_heads][head_dim] dtype; may be q, if q is laid
@@ -678,7 +679,8 @@ size_t ldr_logprobs_workspace_bytes(int32_t batch, int32_t rows, int32_t vocab, 
  * An entry that is -inf has p = 0. A row of nothing else has log p = -inf
  * everywhere and entropy 0; a NaN (which ranks behind every number) or a +inf in a row
  * makes its log p and entropy NaN. Sums are fp32, in an order that depends on the sizes
- * alone. Rows i >= n_rows[b] of the outputs stay as they were.
+ * alone; differences of logits are fp32 before they meet T, infinite beyond its range.
+ * Rows i >= n_rows[b] of the outputs stay as they were.
  *   logits  dev fp32, row (b, i) at logits + (b rows + i) row_stride elements
  *   tokens  dev int32 [batch][rows]
  *   n_rows  dev int32 [batch] (a verification's n_new), or NULL: rows
