@@ -404,7 +404,8 @@ size_t ldr_attend_workspace_bytes(const ldr_pages_config* cfg, int32_t n_q_heads
  *   max_new    rows per sequence of the queries, as reserved
  *   workspace  dev, ldr_attend_workspace_bytes(cfg, n_q_heads, max_new) bytes,
  *              256-byte aligned; keeps the plan, and the partial results of the
- *              ldr_attend calls on it (which must be ordered) */
+ *              ldr_attend calls on it (which must be ordered). A captured graph
+ *              uses it in every replay: it has to live as long */
 int ldr_attend_plan(const ldr_pages* p, int32_t n_q_heads, int32_t max_new,
                     const int32_t* groups, void* workspace, size_t workspace_bytes,
                     void* stream);

@@ -1010,7 +1010,10 @@ template <int BITS, int D> hipError_t launch(const AttendArgs& a, hipStream_t st
   if (e != hipSuccess) return e;
   const int64_t last = (int64_t)a.s.batch * a.w.tiles * a.s.hkv;
   // Few workgroups are bound by their chain of loads: two for the dimensions of 32 rows, unless
-  // one would write over queries that the other reads.
+  // one would write over queries that the other reads. One sequence with 17 rows over 65536
+  // keys, 8 bits: 10.5 us a layer instead of 16.7; 4 with 17 over 16384, two layers, 94 instead
+  // of 98 in all. Two rounds of workgroups are slower: 8 with 17 over 4096 84 instead of 77, 20
+  // with one over 5000 95 instead of 89.
   const char *q = static_cast<const char*>(a.q), *o = static_cast<const char*>(a.o);
   const int64_t rows = (int64_t)a.s.batch * a.max_new;
   const bool apart = o + rows * a.hq * D * 2 <= q || q + rows * a.q_stride * 2 <= o;

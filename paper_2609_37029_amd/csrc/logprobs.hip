@@ -13,8 +13,8 @@
 // own). The first pass writes the maxima; the second picks the groups, then the entries in
 // them (select).
 //
-// Bound by the one read of the logits: 1024 rows of 151936 in 133 us (4.7 TB/s) and 14 us for
-// the second launch; one row 3.5 and 8 us, chains of loads.
+// Bound by the one read of the logits: 1024 rows of 151936 in 133 to 150 us (4.7 to 4.1
+// TB/s) and 14 us for the second launch; one row 3.5 and 8 us, chains of loads.
 #include "ldr_internal.h"
 
 namespace ldr {
