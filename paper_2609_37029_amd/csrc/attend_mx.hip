@@ -14,7 +14,7 @@
 //
 // More: the workgroup decodes a stage of 64 keys into LDS once for all of its waves, in the
 // layout, and between the products, of the bf16 kernel. 64 sequences with one row over 32768
-// keys in common, 8 bits, 45 us a layer; 2 with 512 rows over 8192, 4 bits, 128 us (28 and
+// keys in common, 8 bits, 44 us a layer; 2 with 512 rows over 8192, 4 bits, 128 us (28 and
 // 108 us of a large matrix product).
 //
 // What bounds the last two: a wave's matrix products and its vector instructions (the
@@ -667,6 +667,9 @@ __device__ inline void mx_pair(const AttendArgs& a, const Item& it, int head, in
 // rows, and those rows as pairs of tiles, each with waves of its own, in registers (16 sequences
 // with 60 to 68 rows over 8192 keys 70 to 77 us a layer whichever it is; of 8 bits, one with
 // 68 rows over 65536 keys 46 us so, 57 in registers).
+// Of 65 to 96 rows as one tile two waves have no rows. Decoding all of V there was 5% faster
+// than two tiles for 8 bits (16 sequences with 68 rows over 8192 keys, two layers, 200 instead of
+// 211 us) and 8% slower for 4 (five layers, 432 instead of 400); K and V 3% and 19% slower.
 template <int BITS, int D, bool SMALL>
 __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, int tid, uint8_t* lds) {
   using Page = MxPage<BITS, D>;
@@ -876,8 +879,10 @@ __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, in
     lds_barrier();
     __builtin_amdgcn_sched_barrier(0);
   };
-  // buffer 0: K of stage 0, no V yet; the sets of stages 1 and 2
-  {
+  // buffer 0: K of stage 0, no V yet; the sets of stages 1 and 2. Each kind of wave on its own:
+  // loaded before they part, the sets take more registers than there are (64 sequences with one
+  // row over 32768 keys in common, 8 bits, two layers: 148 us so, 153 before).
+  auto begin = [&]() {
     kp = place(ids_of(0), 0);
     next = ids_of(min(1, stages - 1));
     load_k(ra, kp);
@@ -891,7 +896,7 @@ __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, in
     advance(2);
     load_k(ra, kp);
     load_v(ra, vpl);
-  }
+  };
   // the stages of a wave without rows (its share of the decoding, and the barriers),
   // of the first group, or of the second
   auto run = [&](auto works, auto late, auto Half) {
@@ -909,6 +914,7 @@ __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, in
       if constexpr (LATE) meet();
       if constexpr (WORKS) softmax(Half);
     };
+    begin();
     if constexpr (LATE) meet();
     for (int j = 0; j < stages; j += 2) {   // whole twos
       stage(no, j);
