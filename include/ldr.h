@@ -354,7 +354,8 @@ int ldr_pages_write(ldr_pages* p, int32_t layer, int32_t n_layers, const void* K
  * outside [0, max_rows], is left out whole and sets the sticky LDR_ERANGE flag.
  *   first, n  dev int32 [batch]
  *   K, V      dev [batch][max_rows][n_layers][n_kv_heads][head_dim], of the rows'
- *             type, 16-byte aligned, not over each other (LDR_EINVAL) */
+ *             type, 16-byte aligned; over neither each other, nor first and n,
+ *             nor the cache's pool and state (LDR_EINVAL) */
 int ldr_pages_read(const ldr_pages* p, int32_t layer, int32_t n_layers, const int32_t* first,
                    const int32_t* n, void* K, void* V, int32_t max_rows, void* stream);
 

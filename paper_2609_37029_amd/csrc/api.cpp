@@ -123,11 +123,6 @@ static WsPlan plan_ws(const Shape& s, int batch) {
 
 static bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
-struct Range { const void* p; size_t bytes; };   // p null: none
-static bool overlap(const Range& a, const Range& b) {
-  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
-  return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
-}
 
 }  // namespace ldr
 

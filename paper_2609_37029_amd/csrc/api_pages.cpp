@@ -6,6 +6,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <new>
 
 #include "ldr_internal.h"
@@ -128,10 +129,16 @@ int ldr_pages_read(const ldr_pages* p, int32_t layer, int32_t n_layers, const in
   if (!first || !n || !aligned(first, 4) || !aligned(n, 4)) return LDR_EINVAL;
   if (max_rows < 1 || max_rows > (1 << 28) || !K || !V || !aligned(K, 16) || !aligned(V, 16))
     return LDR_EINVAL;
-  const uintptr_t k = (uintptr_t)K, v = (uintptr_t)V;
-  if ((k < v ? v - k : k - v) < (size_t)p->s.batch * max_rows * n_layers * p->s.hkv * p->s.d * p->s.el)
-    return LDR_EINVAL;      // one over the other
-  return done(launch_pages_read(p->s, p->p, layer, n_layers, first, n, K, V, max_rows,
+  // every workgroup reads the counts, the tables and the pool while others write
+  const PagesShape& s = p->s;
+  const size_t counts = (size_t)s.batch * 4;
+  const size_t rows = (size_t)s.batch * max_rows * n_layers * s.hkv * s.d * s.el;
+  const Range k{K, rows}, v{V, rows};
+  for (const Range& o : {Range{first, counts}, Range{n, counts}, Range{p->p.state, s.words * 4},
+                         Range{p->p.pool, (size_t)2 * s.layers * s.n_pages * s.page_bytes}})
+    if (overlap(k, o) || overlap(v, o)) return LDR_EINVAL;
+  if (overlap(k, v)) return LDR_EINVAL;
+  return done(launch_pages_read(s, p->p, layer, n_layers, first, n, K, V, max_rows,
                                 static_cast<hipStream_t>(stream)));
 }
 

@@ -14,6 +14,13 @@ namespace ldr {
 constexpr size_t kAlign = 256;
 inline size_t align_up(size_t x, size_t a = kAlign) { return (x + a - 1) / a * a; }
 
+// Memory of a call, and whether two have a byte in common.
+struct Range { const void* p; size_t bytes; };   // p null: none
+inline bool overlap(const Range& a, const Range& b) {
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+}
+
 // Byte offsets of the views inside one sequence's arena slot.
 struct Layout {
   size_t kw, vw, m, eta, h;  // region offsets
