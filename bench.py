@@ -21,6 +21,7 @@ from __future__ import annotations
 import argparse
 import json
 import os
+import re
 import statistics
 import sys
 import time
@@ -510,16 +511,33 @@ def cpu_baseline(torch, synth, rig, n_seqs):
 
 # ---- HBM traffic from rocprofv3 counters -----------------------------------------------------
 
+# the sources whose kernels a step launches, and the one that launches them
+STEP_SOURCES = ("api.cpp", "views.hip", "gemm.hip", "draft.hip", "attn.hip", "sample.hip")
+
+
+def step_files(csrc):
+    """STEP_SOURCES and the headers beside them that they include, sorted."""
+    found, todo = set(), list(STEP_SOURCES)
+    while todo:
+        name = todo.pop()
+        if name in found:
+            continue
+        found.add(name)
+        with open(os.path.join(csrc, name)) as fh:
+            todo += [h for h in re.findall(r'^#include "([^"/]+)"', fh.read(), re.M)]
+    return sorted(found)
+
+
 def source_digest():
-    """sha256 over the library sources: counters taken on other sources are stale."""
+    """sha256 over the sources of the drafting step: counters taken on others are stale.
+    The other operators' sources, and the prototypes of the public header, change none of
+    the step's launches."""
     import hashlib
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_2609_37029_amd", "csrc")
-    files = sorted(os.path.join(csrc, f) for f in os.listdir(csrc)
-                   if f.endswith((".hip", ".cpp", ".h")))
-    for f in files + [os.path.join(ROOT, "include", "ldr.h")]:
-        h.update(os.path.basename(f).encode())
-        with open(f, "rb") as fh:
+    for f in step_files(csrc):
+        h.update(f.encode())
+        with open(os.path.join(csrc, f), "rb") as fh:
             h.update(fh.read())
     return h.hexdigest()
 

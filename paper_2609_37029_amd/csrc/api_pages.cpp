@@ -9,7 +9,7 @@
 #include <initializer_list>
 #include <new>
 
-#include "ldr_internal.h"
+#include "serve_internal.h"
 
 namespace ldr {
 

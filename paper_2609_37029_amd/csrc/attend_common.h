@@ -6,7 +6,7 @@
 
 #include <type_traits>
 
-#include "ldr_internal.h"
+#include "serve_internal.h"
 
 namespace ldr {
 namespace {

@@ -15,7 +15,7 @@
 //
 // Bound by the one read of the logits: 1024 rows of 151936 in 133 to 150 us (4.7 to 4.1
 // TB/s) and 14 us for the second launch; one row 3.5 and 8 us, chains of loads.
-#include "ldr_internal.h"
+#include "serve_internal.h"
 
 namespace ldr {
 namespace {

@@ -18,7 +18,7 @@
 #ifndef LDR_MX_H
 #define LDR_MX_H
 
-#include "ldr_internal.h"
+#include "serve_internal.h"
 
 namespace ldr {
 namespace {

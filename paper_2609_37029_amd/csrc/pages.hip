@@ -10,7 +10,7 @@
 // sequences); rows of 64 x 17 tokens 16 us (45 MB in and out, 2.8 TB/s), of 16 x 17 7 us;
 // copies of 64 pages 26 us (84 MB written, 3.2 TB/s, the source in cache); compaction of half
 // the pages of 32 x 4096 rows 6 + 258 us (1.2 GB, 4.7 TB/s).
-#include "ldr_internal.h"
+#include "serve_internal.h"
 
 namespace ldr {
 namespace {

@@ -15,7 +15,7 @@
 // part. 64 sequences of 151936 tokens: sums 18 us (78 MB, 4.3 TB/s), draw 4 us; one: 6
 // and 4. With a workgroup a part of 4096, and without the next part's loads under way,
 // 64 took 56 and 41 us.
-#include "ldr_internal.h"
+#include "serve_internal.h"
 
 namespace ldr {
 namespace {

@@ -2,7 +2,7 @@
 // can be made, and a call that is not refused says LDR_OK.
 #include <hip/hip_runtime.h>
 
-#include "ldr_internal.h"
+#include "serve_internal.h"
 
 namespace ldr {
 hipError_t launch_pages_reset(const PagesShape&, const PagesPtrs&, hipStream_t) { return hipSuccess; }
