@@ -422,9 +422,14 @@ int ldr_attend_plan(const ldr_pages* p, int32_t n_q_heads, int32_t max_new,
  * -inf still multiplies its v by 0. What masked places hold does not count,
  * infinities and NaN included. Rows i >= open[b] of o and lse stay as they were.
  * n_q_heads and max_new are the plan's.
- * A coded cache is attended to as a bf16 cache of the values that its codes stand for
- * (keys near the mask and short runs of keys keep 16 bits of the probabilities, long runs
- * the 8 of a bf16 cache).
+ * A coded cache is attended to as a bf16 cache of the values that its codes stand for, in
+ * which a probability is rounded to bf16 (2^-8 of itself at most) where it meets its v. It
+ * has 2^-16 in two places: in the keys at a sequence's end that are no whole item's (fewer
+ * than 512 of its own, and its open rows), and in items of at most 32 rows of a K/V head
+ * and 1024 keys.
+ * How the plan cuts items follows from the whole batch, and with it the order of a row's
+ * sums and which of its probabilities have the 16 bits: the same call gives the same bits,
+ * and in another batch a row may differ by these roundings.
  *   q    dev dtype (bf16 for a coded cache), row (b, i) at q + (b max_new + i) q_stride elements, its
  *        [n_q_heads][head_dim] contiguous; q_stride a multiple of 8 (bf16) or 4
  *   o    dev [batch][max_new][n_q_heads][head_dim] dtype; may be q, if q is laid

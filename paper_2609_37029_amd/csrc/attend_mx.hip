@@ -190,10 +190,15 @@ __device__ inline void mx_rows(const AttendArgs& a, const Item& it, const SeqInf
   auto id_of = [&](int t) {   // the page of the wave's step t, on its way until it is looked at
     return scalar_word(table, (it.k0 + min(t * W + wave, max(steps - 1, 0)) * kStep) >> shift);
   };
-  // What the rounding of P to bf16 leaves gets a product too in the last kernel, which is bound
-  // by the chain of its loads, and where the waves have few steps, for the same reason: o is
-  // then 0.0017 from its definition (root mean square, relative), its own rounding to bf16,
-  // instead of 0.0023. In longer items it would take 28% more instructions.
+  // What the rounding of P to bf16 leaves gets a product too (P then has 16 bits) in the last
+  // kernel, which is bound by the chain of its loads, and where the waves have few steps, for
+  // the same reason: o is then 0.0017 from its definition (root mean square, relative), its
+  // own rounding to bf16, instead of 0.0023. Without it in any item 8 sequences with 8 rows
+  // over 4096 keys, 4 bits, two layers, take 53 instead of 55 us, the small ones as long. With
+  // it in all of these items 16 sequences with one row over 16384 keys, five layers, take 390
+  // instead of 340, and with it in the others too 16 with 17 rows over 8192 519 instead of 413,
+  // two with 512 over 8192 382 instead of 299: those keep the 8 bits of a bf16 cache. The steps
+  // are those of the plan's cut, so that a row's roundings follow from its batch.
   const bool fine = FINISH || steps <= 4 * W;
   int id = wave < steps ? id_of(0) : 0;
   auto fetch = [&](Raw& x, int t) {
