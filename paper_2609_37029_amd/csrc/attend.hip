@@ -58,12 +58,14 @@ __device__ inline int even_step(int len, int n, int unit) {
 }
 
 // The time of an item of a coded cache, in sixteenths of a whole tile's, and the smallest
-// chunk (of the lightest items, tile.unit keys). Measured, 32 query and 8 K/V heads of 128,
-// 4 bits, all compute units at it, for 1024 keys: up to 32 rows 6.4 us, 64 9.3, 128 17.3,
-// 256 29.4; of 65 to 96 rows two tiles, 4 sixteenths each.
+// chunk (of the lightest items, tile.unit keys). Measured, eight K/V heads, all compute units
+// at it, us for 1024 keys of up to 32 rows, 64, 128, 256: 4 bits, head_dim 128 7, 10, 19, 30
+// (and 65 to 96 rows as two tiles 16, 4 sixteenths each), head_dim 64 3.3, 5.1, 10.7, 21; 8 bits,
+// head_dim 64 5.2, 6.8, 12, 22. With 8 bits and head_dim 128, 14.6, 14.8, 21, 33, the first two
+// are HBM's time with all compute units at it, not a workgroup's: alone they take less.
 constexpr int kMxLeast = 48;
-__device__ inline int mx_weighted(int len, int rows) {
-  const int w = rows <= 32 ? 3 : rows <= 64 ? 5 : rows <= 96 ? 4 : rows <= 128 ? 9 : 16;
+__device__ inline int mx_weighted(int len, int rows, bool two) {
+  const int w = rows <= 32 ? 3 : rows <= 64 ? 5 : two && rows <= 96 ? 4 : rows <= 128 ? 9 : 16;
   return (int)(((long)len * w + 15) / 16);
 }
 
@@ -71,7 +73,7 @@ __device__ inline int mx_weighted(int len, int rows) {
 // sequences for each goes by waves, a sequence at a time. 5.7 us for one sequence, 23 for
 // 64 with 512 pages in common (their tables, 128 KB, through one compute unit): once
 // for all layers.
-// MX: a coded cache, whose items take as long as their rows ask for (mx_weight): a chunk is
+// MX: a coded cache, whose items take as long as their rows ask for (mx_weighted): a chunk is
 // as many sixteenths of a whole tile's keys.
 template <bool BF16, bool MX = false>
 __global__ void __launch_bounds__(kBook)
@@ -95,6 +97,7 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   Item* items = reinterpret_cast<Item*>(ws + w.items);
   constexpr Tile tile = tile_of(BF16);   // divisions by its entries are shifts
   constexpr int least_chunk = MX ? kMxLeast : tile.unit, quantum = MX ? 16 : tile.unit;
+  const bool two = MX && two_tiles(s);
 
   const int all = in ? clamp_rows(s, p.state[s.rows + b]) : 0;
   const int held = in ? min(max(p.state[s.open + b], 0), all) : 0;
@@ -176,8 +179,8 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   const int share = in && members[b] > 1 && common_rows >= kMinShared ? common_rows : 0;
   const int gopen = in ? gopens[b] : 0;
   const int R = open * rep, Rg = share && ld == b ? gopen * rep : 0;    // below 2^28
-  const int otr = tile_rows(tile, MX, R), ot = ceil_div(R, otr);
-  const int gt = ceil_div(Rg, tile_rows(tile, MX, Rg));
+  const int otr = tile_rows(tile, two, R), ot = ceil_div(R, otr);
+  const int gt = ceil_div(Rg, tile_rows(tile, two, Rg));
   int len = open ? tile_keys(rows, open, share, (ot - 1) * otr, rep, tile.unit) : 0;
   if (len < kMinMain) len = 0;
   const int glen = Rg ? share : 0;
@@ -185,7 +188,8 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
   shares[b] = share;
   ends[b] = rows;
   // what the chunks are cut by
-  const int wlen = MX ? mx_weighted(len, R) : len, wglen = MX ? mx_weighted(glen, Rg) : glen;
+  const int wlen = MX ? mx_weighted(len, R, two) : len;
+  const int wglen = MX ? mx_weighted(glen, Rg, two) : glen;
   cuts[b] = float4{(float)ot, (float)wlen, (float)gt, (float)wglen};
   const float mine = wave_sum((float)ot * wlen + (float)gt * wglen);
   if (lane == 0) works[wave] = mine;
@@ -275,12 +279,12 @@ attend_plan_kernel(PagesShape s, PagesPtrs p, int hq, int max_new, const int32_t
       if (i_off[mid] <= t) lo = mid; else hi = mid - 1;
     }
     const int own_rows = opens[lo] * rep;
-    const int own_tiles = ceil_div(own_rows, tile_rows(tile, MX, own_rows));
+    const int own_tiles = ceil_div(own_rows, tile_rows(tile, two, own_rows));
     int k = t - i_off[lo];
     const bool g = k >= own_tiles * o_chunks[lo];
     if (g) k -= own_tiles * o_chunks[lo];
     const int n = g ? gopens[lo] * rep : own_rows;
-    const int tr = tile_rows(tile, MX, n), tiles = ceil_div(n, tr);
+    const int tr = tile_rows(tile, two, n), tiles = ceil_div(n, tr);
     const int c = k / tiles, r0 = (k - c * tiles) * tr;
     const int from = g ? 0 : shares[lo];
     const int keys = g ? shares[lo] : tile_keys(ends[lo], opens[lo], from, r0, rep, tile.unit);

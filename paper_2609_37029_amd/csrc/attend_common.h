@@ -43,11 +43,16 @@ __host__ __device__ constexpr Tile tile_of(bool bf16) {
   return bf16 ? Tile{256, 4 * kStage, 256, 384} : Tile{32, 128, 512, 192};
 }
 __host__ __device__ inline Tile tile_of(const PagesShape& s) { return tile_of(s.dtype != LDR_F32); }
-// Rows of the tiles of a segment of R rows. Of a coded cache 65 to 96 rows are two tiles, of 64
-// rows and of the rest: together 15.7 us for 1024 keys (all compute units at it, 4 bits,
-// head_dim 128), as one 17.3.
-__host__ __device__ inline int tile_rows(const Tile& t, bool mx, int R) {
-  return mx && R > 64 && R <= 96 ? 64 : t.rows;
+// Whether 65 to 96 rows are two tiles, of 64 rows and of the rest. With 4 bits and head_dim 128
+// 16 sequences with 68 rows a K/V head over 8192 keys, five layers, take 408 us so and 419 as
+// one tile; one with 68 over 16384, two layers, 61 and 66; 16 with 96 over 8192 171 and 175. (8
+// with 68 over 4096 76 and 70, 64 over 2000 189 and 179: short ones are slower.) With 8 bits
+// two tiles load and decode twice the bytes: the first 501 and 437, 32 with 72 over 4096 241
+// and 192, none slower as one. With head_dim 64 16 with 80 over 4096, 4 bits, 61 and 60.
+__host__ __device__ inline bool two_tiles(const PagesShape& s) { return s.bits == 4 && s.d == 128; }
+// Rows of the tiles of a segment of R rows.
+__host__ __device__ inline int tile_rows(const Tile& t, bool two, int R) {
+  return two && R > 64 && R <= 96 ? 64 : t.rows;
 }
 // Rounds of items over those workgroups, at most (4 took 2% longer: the
 // grid is sized for as many, and most of it ends at once).
@@ -98,7 +103,7 @@ AttendWs plan_ws(const PagesShape& s, int hq, int max_new) {
   // every tile of the own and of the shared segments once, and the added ones
   const long tiles = ((long)max_new * rep + tile - 1) / tile;
   w.max_items = (int)(s.batch * tiles + rows / tile + s.batch / 2 + added_items(s));
-  if (s.bits) w.max_items += s.batch + s.batch / 2;   // a second tile of 65 to 96 rows
+  if (two_tiles(s)) w.max_items += s.batch + s.batch / 2;   // the second of 65 to 96 rows
   w.tiles = (int)(((long)max_new * rep + kBlock - 1) / kBlock);
   w.blocks = (long)s.batch * w.tiles + rows / kBlock + s.batch / 2 +
              (long)(tile / kBlock) * added_items(s);

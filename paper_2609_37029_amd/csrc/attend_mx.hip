@@ -79,7 +79,7 @@ __device__ inline void join_parts(const AttendArgs& a, const Item& it, const Seq
   // parts: the group's chunks, then the tile's own. Of few rows there are columns
   // to spare: R a part, and 32 / R parts at a time (4 rows of 32 parts, as 64
   // sequences with one token each have, took 8 loads behind one another, 11 us).
-  const int tr = tile_rows(tile_of(a.s), a.s.bits, f.open * a.rep), t = it.r0 / tr * tr;
+  const int tr = tile_rows(tile_of(a.s), two_tiles(a.s), f.open * a.rep), t = it.r0 / tr * tr;
   const int own = f.own_chunks ? ceil_div(tile_keys(f.rows, f.open, f.share, t, a.rep,
                                                     tile_of(a.s).unit), f.step) : 0;
   const int parts = f.grp_chunks + own;
@@ -442,7 +442,7 @@ attend_mx_last_kernel(AttendArgs a) {
   it.q0 = f.qoff;
   const int cbase = f.rows - f.open;
   const Tile tile = tile_of(a.s);
-  const int tr = tile_rows(tile, true, f.open * a.rep), t = it.r0 / tr * tr;
+  const int tr = tile_rows(tile, two_tiles(a.s), f.open * a.rep), t = it.r0 / tr * tr;
   it.k0 = f.share + (f.own_chunks ? tile_keys(f.rows, f.open, f.share, t, a.rep, tile.unit) : 0);
   it.k1 = cbase + (it.r0 + it.nr - 1) / a.rep + 1;
   mx_rows<BITS, D, true, W, NPL>(a, it, f, cbase, head, (int)blockIdx.x % SPLIT * NPL,
@@ -672,9 +672,9 @@ __device__ inline void mx_pair(const AttendArgs& a, const Item& it, int head, in
 // rows, and those rows as pairs of tiles, each with waves of its own, in registers (16 sequences
 // with 60 to 68 rows over 8192 keys 70 to 77 us a layer whichever it is; of 8 bits, one with
 // 68 rows over 65536 keys 46 us so, 57 in registers).
-// Of 65 to 96 rows as one tile two waves have no rows. Decoding all of V there was 5% faster
-// than two tiles for 8 bits (16 sequences with 68 rows over 8192 keys, two layers, 200 instead of
-// 211 us) and 8% slower for 4 (five layers, 432 instead of 400); K and V 3% and 19% slower.
+// Of 65 to 96 rows as one tile two waves have no rows, and decode their share like the others (8
+// bits, 16 sequences with 68 rows over 8192 keys, two layers: 183 us; all of V left to those two
+// 200, K and V 217).
 template <int BITS, int D, bool SMALL>
 __device__ inline void mx_wide(const AttendArgs& a, const Item& it, int head, int tid, uint8_t* lds) {
   using Page = MxPage<BITS, D>;
