@@ -389,6 +389,7 @@ attend_rows_kernel(AttendArgs a) {
     // parts: the group's chunks, then the tile's own. Of few rows there are columns
     // to spare: R a part, and 32 / R parts at a time (4 rows of 32 parts, as 64
     // sequences with one token each have, took 8 loads behind one another, 11 us).
+    // join_parts (attend_mx.hip) does the same for coded caches.
     const int t = it.r0 / tile_of(a.s).rows * tile_of(a.s).rows;
     const int own = f.own_chunks
                         ? (tile_keys(f.rows, f.open, f.share, t, a.rep, tile_of(a.s).unit) + f.step - 1) / f.step : 0;

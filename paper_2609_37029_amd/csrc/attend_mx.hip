@@ -24,6 +24,11 @@
 // them; one wave a SIMD, with 512 registers and nothing waiting in LDS, was slower still (a
 // lone wave issues a vector instruction every 5 to 9 cycles, two one every 4.3).
 //
+// Two waves a SIMD have 256 registers each. With head_dim 128 the 8-bit kernel spills 6 of
+// them, 11 with pages of 32 rows (4 bits 0 and 4), its last kernel 8 with eight waves and 3
+// with four (4 bits none; with half of the dimensions a workgroup none); head_dim 64 none. What
+// these cost was not measured.
+//
 // K and q may be taken along head_dim in any order that is the same for both, keys in any
 // order that is the same for P and V, and the dimensions of O in any order that all parts
 // share: tile t of O^T has the dimensions 64 (t / 2) + 2 r + t % 2 in its rows r, so that
@@ -67,6 +72,9 @@ __device__ inline float value_of_v(const MxPage<BITS, D>& p, int row, int dim) {
   return mx_value<BITS>(code, *p.vscale(dim / kMxBlock, row));
 }
 
+// attend_rows_kernel (attend.hip) joins the parts of uncoded caches by the same steps and the
+// same places, written out there since as a function it rounds otherwise: a change of where
+// parts lie, or of how few rows share the columns, is one to both.
 // Into a wave's o, m and l (column col: row it.r0 + col of sequence it.seq): the parts of
 // its rows, which W waves take in turn; l in the first half alone. Of O^T the 2 NPL tiles
 // from pair p0 of them on, U parts on their way at a time.
