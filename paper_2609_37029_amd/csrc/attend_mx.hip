@@ -8,14 +8,15 @@
 // Items of up to 32 rows (a token a sequence): every wave takes steps of 32 keys of its
 // own and decodes them into the operands of its products; nothing waits for another
 // wave until the end. Bound by HBM: 16 sequences with one row over 16384 keys, 32 query and 8
-// K/V heads of 128, 4 bits, 58 us a layer (280 MB, 4.8 TB/s); with all keys in cache 48.
+// K/V heads of 128, 4 bits, 60 us a layer (280 MB, 4.7 TB/s), 48 with all keys in cache; 8 bits
+// 103 (540 MB, 5.3 TB/s).
 //
 // Up to 64 rows: the same with two tiles of rows a wave.
 //
 // More: the workgroup decodes a stage of 64 keys into LDS once for all of its waves, in the
 // layout, and between the products, of the bf16 kernel. 64 sequences with one row over 32768
-// keys in common, 8 bits, 44 us a layer; 2 with 512 rows over 8192, 4 bits, 128 us (28 and
-// 108 us of a large matrix product).
+// keys in common, 8 bits, 41 us a layer; 2 with 512 rows over 8192, 4 bits, 124 us, 8 bits 131
+// (28 and 108 us of a large matrix product).
 //
 // What bounds the last two: a wave's matrix products and its vector instructions (the
 // exponentials and their neighbours, 110 a tile and step of 32 keys, and 130 of decoding) take
@@ -679,7 +680,7 @@ __device__ inline void mx_pair(const AttendArgs& a, const Item& it, int head, in
 // waited for: with all keys in cache 68 rows take as long), stages of 128 keys for up to 128
 // rows, and those rows as pairs of tiles, each with waves of its own, in registers (16 sequences
 // with 60 to 68 rows over 8192 keys 70 to 77 us a layer whichever it is; of 8 bits, one with
-// 68 rows over 65536 keys 46 us so, 57 in registers).
+// 68 rows over 65536 keys 42 us so, 57 in registers).
 // Of 65 to 96 rows as one tile two waves have no rows, and decode their share like the others (8
 // bits, 16 sequences with 68 rows over 8192 keys, two layers: 183 us; all of V left to those two
 // 200, K and V 217).
@@ -1029,10 +1030,11 @@ template <int BITS, int D> hipError_t launch(const AttendArgs& a, hipStream_t st
   if (e != hipSuccess) return e;
   const int64_t last = (int64_t)a.s.batch * a.w.tiles * a.s.hkv;
   // Few workgroups are bound by their chain of loads: two for the dimensions of 32 rows, unless
-  // one would write over queries that the other reads. One sequence with 17 rows over 65536
-  // keys, 8 bits: 10.5 us a layer instead of 16.7; 4 with 17 over 16384, two layers, 94 instead
-  // of 98 in all. Two rounds of workgroups are slower: 8 with 17 over 4096 84 instead of 77, 20
-  // with one over 5000 95 instead of 89.
+  // one would write over queries that the other reads. 32 query and 8 K/V heads, two layers: one
+  // sequence with 17 rows over 65536 keys, 8 bits, 115 us instead of 124, 4 with 17 over 16384, 4
+  // bits, 92 instead of 98, 16 with one over 16384, 8 bits, 234 instead of 244. Two rounds of
+  // workgroups are slower: 4 bits, 8 with 17 over 4096 84 instead of 77, 20 with one over 5000 95
+  // instead of 88 (but 6 with 17 over 4096, 8 bits, 68 instead of 75).
   const char *q = static_cast<const char*>(a.q), *o = static_cast<const char*>(a.o);
   const int64_t rows = (int64_t)a.s.batch * a.max_new;
   const bool apart = o + rows * a.hq * D * 2 <= q || q + rows * a.q_stride * 2 <= o;

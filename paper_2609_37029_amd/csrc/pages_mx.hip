@@ -7,8 +7,9 @@
 // rows' bytes or a half, are what goes through LDS.
 //
 // Bound by HBM. Measured, Qwen3-8B heads, five layers, pages of 64: 1536 rows of each of two
-// sequences into 8 bits 23 us (95 MB in and out, 4.2 TB/s) and back 20 us; 16 x 13 rows into 4
-// bits 7 us and back 5; 49000 rows of 4 bits out 285 us (1.3 GB, 4.5 TB/s).
+// sequences into 8 bits 22 us (95 MB in and out, 4.3 TB/s) and back 20 us; 16 x 13 rows into 4
+// bits 7 us and back 5; 49700 rows of 4 bits out 283 us (1.3 GB, 4.6 TB/s), of 8 bits 305 (1.5 GB,
+// 5.1 TB/s), of bf16 376 (2.0 GB, 5.4 TB/s), of fp32 795 (4.1 GB, 5.1 TB/s).
 #include "mx.h"
 
 namespace ldr {
